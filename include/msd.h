@@ -21,6 +21,15 @@
  *   msd_reuse_select     Sec. 3.1 reuse criterion and next-window selection,
  *                        App. E fallback statistics.
  *
+ * and the serving operators around it:
+ *
+ *   msd_paged_append     keys and values into a paged cache (bf16, or 8 bits
+ *                        with block scales), the keys rotated on the way;
+ *   msd_paged_commit     the accepted path of a block into it (Sec. 2 commit);
+ *   msd_paged_attention  attention of a block's rows over it, with a sliding
+ *                        window and sinks;
+ *   msd_sample           tokens under temperature, top-k, top-p and min-p.
+ *
  * Conventions
  *  - Every pointer marked "device" is HIP device memory owned by the caller;
  *    "host" pointers are read during the call only. The library never takes
@@ -68,6 +77,7 @@ typedef enum {
 #define MSD_DEV_CAPACITY 1u  /* len[b] + n_slots > capacity                    */
 #define MSD_DEV_CANDIDATE 2u /* REJECTION: child token without draft mass      */
 #define MSD_DEV_TOKEN 4u     /* a block token outside [0, vocab)               */
+#define MSD_DEV_PAGE 8u      /* a page id outside [0, n_pages)                 */
 
 /* Thread-local text of the last non-OK status returned on this thread. */
 const char* msd_last_error(void);
@@ -378,6 +388,176 @@ msd_status msd_reuse_select(const msd_model* model, const msd_block* block, cons
                             const float* logits, const float* lse, const int32_t* ee_ids,
                             int32_t kappa, int32_t* next_case, int32_t* next_node, float* omega,
                             msd_reuse_stats* stats, hipStream_t stream);
+
+/*
+ * ---------------------------------------------------------------------------
+ * Paged key/value cache
+ * ---------------------------------------------------------------------------
+ * Positions of sequence b live in pages of page_size tokens: position p in
+ * page page_table[b][p / page_size] at row p % page_size, the same page ids in
+ * every layer. k and v are device [n_layers][n_pages][n_kv_heads][page_size]
+ * [head_dim]:
+ *  MSD_KV_BF16  bf16;
+ *  MSD_KV_FP8   8-bit floats (e4m3: 4 exponent, 3 fraction bits, no infinity,
+ *               largest 448) with one scale for each block of
+ *               MSD_KV_SCALE_TOKENS consecutive tokens and kv head:
+ *               k_scale / v_scale, device uint8 [n_layers][n_pages]
+ *               [n_kv_heads][page_size / 16], value = code * 2^(scale - 127).
+ * The scale of a block is the smallest power of two, at least 2^-127, with
+ * every finite magnitude in the block at most 448 times it: rows appended to
+ * a half-filled block raise it where they have to, and the codes already
+ * there are then re-coded by the ratio, a pure change of exponent (exact but
+ * for codes that fall below 2^-6). Infinities are stored as the largest
+ * value, NaN as NaN.
+ * len[b] = committed positions of sequence b. Page ids are read only for
+ * positions that a call touches; one outside [0, n_pages) sets MSD_DEV_PAGE
+ * (append and commit: that block's rows are not stored; attention: its keys
+ * are left out). Sequences may share pages that they only read. A block of
+ * 16 tokens that one call writes belongs to one sequence.
+ * Limits: head_dim in {64, 128}; page_size in {16, 32, 64, 128, 256};
+ * max_pages * page_size <= 2^30.
+ */
+enum { MSD_KV_BF16 = 0, MSD_KV_FP8 = 1 };
+#define MSD_KV_SCALE_TOKENS 16
+typedef struct {
+  void* k;
+  void* v;
+  uint8_t* k_scale;            /* MSD_KV_FP8 only                             */
+  uint8_t* v_scale;
+  const int32_t* page_table;   /* device [batch_cap][max_pages]               */
+  int32_t* len;                /* device [batch_cap]                          */
+  uint32_t* status;            /* device word; kernels OR MSD_DEV_* codes in  */
+  int32_t format, n_layers, n_pages, n_kv_heads, page_size, head_dim;
+  int32_t batch_cap, max_pages;
+} msd_paged_kv;
+
+/* Position rotation of the first rotary_dim dims of a head (a multiple of 16,
+ * at most head_dim): the pair (a, b) becomes (a c - b s, b c + a s) with
+ * (c, s) = table[position][j], in fp32. Pairs j: dims (j, j + rotary_dim / 2)
+ * (MSD_ROPE_HALF) or (2 j, 2 j + 1) (MSD_ROPE_INTERLEAVED). The table holds
+ * (cos, sin) of position times frequency, whatever scaling for long contexts
+ * the caller's frequencies have, and covers max_pages * page_size positions. */
+enum { MSD_ROPE_HALF = 0, MSD_ROPE_INTERLEAVED = 1 };
+typedef struct {
+  const float* table;          /* device fp32 [positions][rotary_dim / 2][2]  */
+  int32_t positions, rotary_dim, layout;
+} msd_rope;
+
+/* New rows of keys and values: element (layer l, sequence b, row r, kv head h,
+ * dim d) of k at k + l * layer_stride + b * seq_stride + r * row_stride +
+ * h * head_stride + d, v alike. Strides in elements, >= 0, multiples of 8;
+ * pointers 16-byte aligned. */
+typedef struct {
+  const void* k;               /* device bf16                                 */
+  const void* v;
+  int64_t layer_stride, seq_stride, row_stride, head_stride;
+  int32_t layer, n_layers;     /* the rows go to layers layer .. + n_layers-1 */
+  int32_t batch, n_rows;       /* batch <= batch_cap, n_rows >= 1             */
+  const int32_t* count;        /* device [batch]: the first count[b] rows of
+                                  sequence b (clamped to [0, n_rows]); NULL:
+                                  all n_rows                                  */
+} msd_kv_rows;
+
+/*
+ * Writes row r of sequence b at position len[b] + r, the key rotated there
+ * when rope is non-NULL. len is not changed: a decoder appends layer by layer
+ * at the same positions and adds the counts once all layers are written. A
+ * sequence that would pass max_pages * page_size sets MSD_DEV_CAPACITY and
+ * none of its rows are stored.
+ */
+msd_status msd_paged_append(const msd_paged_kv* kv, const msd_kv_rows* rows, const msd_rope* rope,
+                            hipStream_t stream);
+
+/*
+ * Commit / rollback (Sec. 2) of a block whose keys and values were kept beside
+ * the cache: rows path[b][0 .. A_b] of sequence b (A_b = acc_len[b], the
+ * outputs of msd_accept; n_rows = n_slots, count NULL) are written at
+ * positions len[b] .. len[b] + A_b, then len[b] += 1 + A_b. Rejected rows
+ * never reach a page or its scales. A sequence with A_b outside [0, n_rows)
+ * is left as it was; path entries are clamped to [0, n_rows). The rows cover
+ * all layers of the cache (layer 0, n_layers).
+ */
+msd_status msd_paged_commit(const msd_paged_kv* kv, const msd_kv_rows* rows, const msd_rope* rope,
+                            const int32_t* acc_len, const int32_t* path, hipStream_t stream);
+
+/*
+ * Attention of a block's rows over one layer of the paged cache. Slot i of
+ * sequence b sits at position P(i) = len[b] + depth(i) and attends, per query
+ * head h with the keys of kv head h / (n_heads / n_kv_heads), to
+ *  k_new non-NULL  the cached positions [0, len[b]) and the block's own rows
+ *                  k_new / v_new, slot j seen by i when it is i or an ancestor
+ *                  of i (parent as in msd_block; NULL: a chain);
+ *  k_new NULL      the cached positions [0, P(i)], the block's own rows having
+ *                  been appended at len[b] + slot (a chain: parent NULL).
+ * window > 0 keeps only keys at positions p with P(i) - p < window or
+ * p < sinks (0: all). The output is softmax(scale * q k) v in fp32, rounded
+ * once to bf16. rope rotates q, and k_new, at their positions.
+ * count (device [batch], NULL: n_slots): only the first count[b] slots of
+ * sequence b are rows (clamped to [0, n_slots]); the others are neither read
+ * nor written. A sequence with len[b] < 0 or len[b] + n_slots past
+ * max_pages * page_size sets MSD_DEV_CAPACITY and its outputs are left as
+ * they were. Infinities and NaN in keys and values that a row does not see do
+ * not reach it.
+ * Strides in elements, >= 0, multiples of 8; pointers 16-byte aligned; out
+ * overlaps no input. n_slots in [1, 64], n_heads % n_kv_heads == 0,
+ * ws of msd_paged_attention_workspace_bytes (it never falls when an argument
+ * grows), 16-byte aligned.
+ */
+typedef struct {
+  const void* q;               /* device bf16 (seq, row, head, dim)           */
+  int64_t q_seq, q_row, q_head;
+  void* out;                   /* device bf16                                 */
+  int64_t out_seq, out_row, out_head;
+  const void* k_new;           /* device bf16 or NULL                         */
+  const void* v_new;
+  int64_t new_seq, new_row, new_head;
+  const int32_t* parent;       /* host [n_slots] or NULL                      */
+  const int32_t* count;        /* device [batch] or NULL                      */
+  const msd_rope* rope;        /* host struct or NULL                         */
+  float scale;                 /* finite                                      */
+  int32_t batch, n_slots, n_heads, window, sinks;
+} msd_paged_attn;
+size_t msd_paged_attention_workspace_bytes(const msd_paged_kv* kv, int32_t batch, int32_t n_slots,
+                                           int32_t n_heads);
+msd_status msd_paged_attention(const msd_paged_kv* kv, int32_t layer, const msd_paged_attn* attn,
+                               void* ws, size_t ws_bytes, hipStream_t stream);
+
+/*
+ * Tokens from rows of logits, one uniform each. Per row, in this order:
+ *  temperature  p = Softmax(z / T) (T <= 0 or NaN: greedy, the most likely
+ *               token); NaN logits count as -inf, +inf as the largest fp32;
+ *  top_k        only the k most likely tokens, ties to the smaller id
+ *               (k <= 0: all);
+ *  top_p        of those, renormalised, the smallest set of most likely
+ *               tokens (ties to the smaller id) with mass >= top_p; one at
+ *               least (top_p >= 1 or NaN: all);
+ *  min_p        of those, tokens with p >= min_p * max p (min_p <= 0 or NaN:
+ *               all; the most likely one always stays).
+ * tok is the first id, ascending, whose cumulative mass over the kept tokens
+ * exceeds u * total: the inverse CDF of msd_accept (u outside [0, 1) is
+ * clamped to it). logp is its log-probability in the kept, renormalised law,
+ * kept the number of kept tokens. A row without a logit above -inf gives
+ * tok -1, logp -inf, kept 0.
+ * Masses are 64-bit fixed point, 2^-43 of the most likely token's a step, from
+ * fp64 exponentials: sums do not depend on their order, so the same inputs
+ * give the same token on every run. Tokens under half a step draw nothing.
+ * With every block row sampled, tok is the argmax argument of msd_accept's
+ * MSD_GREEDY walk: sample-and-compare (Sec. 3.1) under the filtered laws.
+ */
+typedef struct {
+  const float* temperature;    /* device [rows] or NULL (1)                   */
+  const int32_t* top_k;        /* device [rows] or NULL (all)                 */
+  const float* top_p;          /* device [rows] or NULL (all)                 */
+  const float* min_p;          /* device [rows] or NULL (all)                 */
+} msd_sample_params;
+size_t msd_sample_workspace_bytes(int32_t rows, int32_t vocab);
+/* logits device fp32, row r at logits + r * row_stride (row_stride >= vocab);
+ * u device fp32 [rows]; tok device int32 [rows]; logp (fp32) and kept (int32)
+ * device [rows] or NULL; params NULL: all defaults. rows in [1, 65535],
+ * vocab in [1, 1048576]. */
+msd_status msd_sample(const float* logits, int64_t row_stride, int32_t rows, int32_t vocab,
+                      const msd_sample_params* params, const float* u, int32_t* tok, float* logp,
+                      int32_t* kept, void* ws, size_t ws_bytes, hipStream_t stream);
 
 /*
  * Instrumentation (benchmarking only): when set, msd_verify_block times the

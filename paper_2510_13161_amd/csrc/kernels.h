@@ -275,4 +275,79 @@ struct ReuseArgs {
 };
 hipError_t launch_reuse(const ReuseArgs& a, hipStream_t s);
 
+// ---------------------------------------------------------------------------
+// paged key/value cache (msd_paged_kv): append, commit, attention
+// ---------------------------------------------------------------------------
+constexpr int kScaleTokens = 16;      // tokens of a scale block (8-bit pages)
+constexpr float kCodeMax = 448.0f;    // largest e4m3 magnitude
+
+struct RopeView {
+  const float2* table;     // [positions][rd / 2] (cos, sin), or null
+  int32_t rd;              // rotated dims
+  int32_t interleaved;     // pairs (2 j, 2 j + 1) instead of (j, j + rd / 2)
+};
+
+struct PagedView {
+  void* k;                 // [n_layers][n_pages][heads][page][hd]: bf16 or e4m3 codes
+  void* v;
+  uint8_t* k_scale;        // [n_layers][n_pages][heads][page / 16] or null (bf16)
+  uint8_t* v_scale;
+  const int32_t* page_table;  // [batch_cap][max_pages]
+  int32_t* len;
+  uint32_t* status;
+  int32_t n_pages, heads, page_shift, head_dim, max_pages;
+  int64_t capacity;        // max_pages << page_shift
+};
+
+struct AppendArgs {
+  PagedView kv;
+  RopeView rope;
+  const uint16_t* k;
+  const uint16_t* v;
+  int64_t layer_stride, seq_stride, row_stride, head_stride;
+  int32_t layer, n_layers, batch, n_rows;
+  const int32_t* count;    // append: rows of each sequence, or null
+  const int32_t* acc_len;  // commit: accepted drafts, or null
+  const int32_t* path;     // commit: [batch][n_rows] slots
+};
+hipError_t launch_paged_append(bool fp8, const AppendArgs& a, hipStream_t s);
+// commit: len[b] += 1 + acc_len[b] (after launch_paged_append, same args)
+hipError_t launch_paged_advance(const AppendArgs& a, hipStream_t s);
+
+struct PagedAttnArgs {
+  PagedView kv;
+  int32_t layer;
+  RopeView rope;
+  const uint16_t* q;
+  int64_t q_seq, q_row, q_head;
+  uint16_t* out;
+  int64_t out_seq, out_row, out_head;
+  const uint16_t* k_new;   // or null: the block's rows are in the pages
+  const uint16_t* v_new;
+  int64_t new_seq, new_row, new_head;
+  const int32_t* count;    // [batch] or null
+  float scale;
+  int32_t batch, n_slots, n_heads, window, sinks;
+  Topo topo;
+};
+hipError_t launch_paged_attention(bool fp8, const PagedAttnArgs& a, hipStream_t s);
+
+// ---------------------------------------------------------------------------
+// sampling
+// ---------------------------------------------------------------------------
+struct SampleArgs {
+  const float* logits;
+  int64_t row_stride;
+  int32_t rows, vocab;
+  const float* temperature;  // [rows] or null, likewise the next three
+  const int32_t* top_k;
+  const float* top_p;
+  const float* min_p;
+  const float* u;
+  int32_t* tok;
+  float* logp;               // or null
+  int32_t* kept;             // or null
+};
+hipError_t launch_sample(const SampleArgs& a, hipStream_t s);
+
 }  // namespace msd

@@ -12,6 +12,7 @@
 #include "kernels.h"
 #include "msd.h"
 #include "plan.h"
+#include "serve.h"
 
 using namespace msd;
 
@@ -288,6 +289,15 @@ msd_status verify_launch(const msd_model* m, msd_kv_cache* kv, const msd_block* 
                          char* w, const Topo& topo, const Layout& L, hipStream_t stream);
 
 }  // namespace
+
+// The error text of the entry points in other files.
+msd_status msd::report(msd_status s, const char* msg) noexcept {
+  try {
+    g_err = msg;
+  } catch (...) {  // no memory for the text: the status alone
+  }
+  return s;
+}
 
 extern "C" {
 

@@ -19,7 +19,7 @@ LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libmsd.so")
 MSD_OK = 0
 MSD_ERR_INVALID_ARG, MSD_ERR_SHAPE, MSD_ERR_CAPACITY = -1, -2, -3
 MSD_ERR_UNSUPPORTED, MSD_ERR_WORKSPACE, MSD_ERR_HIP = -4, -5, -6
-MSD_DEV_CAPACITY, MSD_DEV_CANDIDATE, MSD_DEV_TOKEN = 1, 2, 4
+MSD_DEV_CAPACITY, MSD_DEV_CANDIDATE, MSD_DEV_TOKEN, MSD_DEV_PAGE = 1, 2, 4, 8
 MSD_NORM_RMS, MSD_NORM_LAYER = 0, 1
 MSD_ACT_SWIGLU, MSD_ACT_RELU = 0, 1
 MSD_POS_ROPE, MSD_POS_LEARNED = 0, 1
@@ -32,12 +32,18 @@ LAYER_SLOTS = ["attn_norm.g", "attn_norm.b", "wq", "wk", "wv", "bq", "bk", "bv",
 
 EXPORTED = ["msd_last_error", "msd_model_create", "msd_model_destroy", "msd_workspace_bytes",
             "msd_verify_block", "msd_early_exit_topk", "msd_accept", "msd_kv_commit",
-            "msd_reuse_select", "msd_set_profile", "msd_verify_block_static"]
+            "msd_reuse_select", "msd_set_profile", "msd_verify_block_static",
+            "msd_paged_append", "msd_paged_commit", "msd_paged_attention",
+            "msd_paged_attention_workspace_bytes", "msd_sample", "msd_sample_workspace_bytes"]
 MSD_STATIC_SCRATCH_BYTES = 64 << 20
 MSD_ACCEPT_WS_PER_ROW = 1024  # bytes a row of the acceptance workspace (msd.h)
 MSD_K_QKV, MSD_K_ATTN, MSD_K_OPROJ, MSD_K_FFN_UP, MSD_K_FFN_DOWN = 0, 1, 2, 3, 4
 MSD_NEXT_BRANCH, MSD_NEXT_CONTINUE, MSD_NEXT_FRESH = 0, 1, 2
 MSD_MAX_TREE_NODES = 256
+MSD_KV_BF16, MSD_KV_FP8 = 0, 1
+MSD_KV_SCALE_TOKENS = 16
+MSD_ROPE_HALF, MSD_ROPE_INTERLEAVED = 0, 1
+ROPE_LAYOUTS = {"half": MSD_ROPE_HALF, "interleaved": MSD_ROPE_INTERLEAVED}
 
 
 class MsdError(RuntimeError):
@@ -88,6 +94,42 @@ class ReuseStats(ctypes.Structure):
                 ("omega_sum", ctypes.c_double)]
 
 
+class PagedKV(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in
+                ("k", "v", "k_scale", "v_scale", "page_table", "len", "status")] + \
+               [(n, ctypes.c_int32) for n in
+                ("format", "n_layers", "n_pages", "n_kv_heads", "page_size", "head_dim",
+                 "batch_cap", "max_pages")]
+
+
+class Rope(ctypes.Structure):
+    _fields_ = [("table", ctypes.c_void_p), ("positions", ctypes.c_int32),
+                ("rotary_dim", ctypes.c_int32), ("layout", ctypes.c_int32)]
+
+
+class KVRows(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p)] + \
+               [(n, ctypes.c_int64) for n in
+                ("layer_stride", "seq_stride", "row_stride", "head_stride")] + \
+               [(n, ctypes.c_int32) for n in ("layer", "n_layers", "batch", "n_rows")] + \
+               [("count", ctypes.c_void_p)]
+
+
+class PagedAttn(ctypes.Structure):
+    _fields_ = [("q", ctypes.c_void_p), ("q_seq", ctypes.c_int64), ("q_row", ctypes.c_int64),
+                ("q_head", ctypes.c_int64), ("out", ctypes.c_void_p), ("out_seq", ctypes.c_int64),
+                ("out_row", ctypes.c_int64), ("out_head", ctypes.c_int64),
+                ("k_new", ctypes.c_void_p), ("v_new", ctypes.c_void_p), ("new_seq", ctypes.c_int64),
+                ("new_row", ctypes.c_int64), ("new_head", ctypes.c_int64),
+                ("parent", ctypes.POINTER(ctypes.c_int32)), ("count", ctypes.c_void_p),
+                ("rope", ctypes.POINTER(Rope)), ("scale", ctypes.c_float)] + \
+               [(n, ctypes.c_int32) for n in ("batch", "n_slots", "n_heads", "window", "sinks")]
+
+
+class SampleParams(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("temperature", "top_k", "top_p", "min_p")]
+
+
 _lib = None
 
 
@@ -113,12 +155,46 @@ def lib() -> ctypes.CDLL:
         L.msd_kv_commit.argtypes = [P, P, P, P, P, P]
         L.msd_set_profile.argtypes = [P, i32, P, P, i32]
         L.msd_reuse_select.argtypes = [P, P, P, P, P, P, P, P, P, i32, P, P, P, P, P]
+        L.msd_paged_append.argtypes = [P, P, P, P]
+        L.msd_paged_commit.argtypes = [P, P, P, P, P, P]
+        L.msd_paged_attention.argtypes = [P, i32, P, P, ctypes.c_size_t, P]
+        L.msd_paged_attention_workspace_bytes.argtypes = [P, i32, i32, i32]
+        L.msd_paged_attention_workspace_bytes.restype = ctypes.c_size_t
+        L.msd_sample.argtypes = [P, ctypes.c_int64, i32, i32, P, P, P, P, P, P, ctypes.c_size_t, P]
+        L.msd_sample_workspace_bytes.argtypes = [i32, i32]
+        L.msd_sample_workspace_bytes.restype = ctypes.c_size_t
         for f in ("msd_model_create", "msd_verify_block", "msd_verify_block_static",
                   "msd_early_exit_topk", "msd_accept",
-                  "msd_kv_commit", "msd_reuse_select", "msd_set_profile"):
+                  "msd_kv_commit", "msd_reuse_select", "msd_set_profile", "msd_paged_append",
+                  "msd_paged_commit", "msd_paged_attention", "msd_sample"):
             getattr(L, f).restype = ctypes.c_int
         _lib = L
     return _lib
+
+
+def _need(ok: bool, what: str) -> None:
+    """A call whose tensors do not fit its arguments: refused before the library sees addresses."""
+    if not ok:
+        raise MsdError(MSD_ERR_INVALID_ARG, what)
+
+
+def _typed(t: torch.Tensor, dtype, shape, what: str) -> torch.Tensor:
+    _need(isinstance(t, torch.Tensor) and t.dtype == dtype and tuple(t.shape) == tuple(shape) and t.is_cuda and
+          t.is_contiguous(), f"{what}: a contiguous device {dtype} tensor of shape {tuple(shape)}")
+    return t
+
+
+def _fits(kv, rows) -> None:
+    """Rows of another head layout than the pages', or tensors of another device than the current one."""
+    heads, hd = getattr(rows, "_heads", (None, kv.head_dim))
+    _need(heads in (None, kv.n_kv_heads) and hd == kv.head_dim, "rows and pages differ in kv heads or head_dim")
+    for x in (kv, rows):
+        _need(getattr(x, "_device", torch.cuda.current_device()) == torch.cuda.current_device(),
+              "tensors of another device than the current one")
+
+
+def _nbytes(ws: torch.Tensor) -> int:
+    return ws.numel() * ws.element_size()
 
 
 def last_error() -> str:
@@ -233,6 +309,58 @@ def set_profile(handle, kclass: int, begin_events, end_events) -> None:
     _check(lib().msd_set_profile(handle, kclass, B if n else None, E if n else None, n))
 
 
+def paged_append(kv: PagedKV, rows: KVRows, rope: Optional[Rope] = None, stream=None) -> None:
+    _fits(kv, rows)
+    _check(lib().msd_paged_append(ctypes.byref(kv), ctypes.byref(rows),
+                                  ctypes.byref(rope) if rope is not None else None,
+                                  _stream(stream)))
+
+
+def paged_commit(kv: PagedKV, rows: KVRows, acc_len, path, rope: Optional[Rope] = None,
+                 stream=None) -> None:
+    """acc_len: device int32 [batch], path: device int32 [batch][n_rows], as accept wrote them."""
+    _fits(kv, rows)
+    _typed(acc_len, torch.int32, (rows.batch,), "acc_len")
+    _typed(path, torch.int32, (rows.batch, rows.n_rows), "path")
+    _check(lib().msd_paged_commit(ctypes.byref(kv), ctypes.byref(rows),
+                                  ctypes.byref(rope) if rope is not None else None, _ptr(acc_len),
+                                  _ptr(path), _stream(stream)))
+
+
+def paged_attention_workspace_bytes(kv: PagedKV, batch: int, n_slots: int, n_heads: int) -> int:
+    return int(lib().msd_paged_attention_workspace_bytes(ctypes.byref(kv), batch, n_slots, n_heads))
+
+
+def paged_attention(kv: PagedKV, layer: int, attn: PagedAttn, ws: torch.Tensor, stream=None) -> None:
+    _fits(kv, attn)
+    _check(lib().msd_paged_attention(ctypes.byref(kv), layer, ctypes.byref(attn), _ptr(ws),
+                                     _nbytes(ws), _stream(stream)))
+
+
+def sample_workspace_bytes(rows: int, vocab: int) -> int:
+    return int(lib().msd_sample_workspace_bytes(rows, vocab))
+
+
+def sample(logits: torch.Tensor, u: torch.Tensor, params: Optional[SampleParams], tok: torch.Tensor,
+           ws: torch.Tensor, logp: Optional[torch.Tensor] = None,
+           kept: Optional[torch.Tensor] = None, stream=None) -> None:
+    """logits: device fp32 [rows][vocab], rows contiguous (any row stride >= vocab)."""
+    _need(logits.dim() == 2 and logits.dtype == torch.float32 and logits.is_cuda and
+          (logits.stride(1) == 1 or logits.shape[1] == 1), "logits: a device fp32 [rows][vocab] tensor of contiguous rows")
+    rows, vocab = logits.shape
+    _typed(u, torch.float32, (rows,), "u")
+    _typed(tok, torch.int32, (rows,), "tok")
+    if logp is not None:
+        _typed(logp, torch.float32, (rows,), "logp")
+    if kept is not None:
+        _typed(kept, torch.int32, (rows,), "kept")
+    _need(params is None or getattr(params, "_rows", None) in (None, rows), "params: one value for each row of logits")
+    _need(logits.device.index == torch.cuda.current_device(), "tensors of another device than the current one")
+    _check(lib().msd_sample(logits.data_ptr(), logits.stride(0) if rows > 1 else vocab, rows, vocab,
+                            ctypes.byref(params) if params is not None else None, _ptr(u), _ptr(tok),
+                            _ptr(logp), _ptr(kept), _ptr(ws), _nbytes(ws), _stream(stream)))
+
+
 # ---------------------------------------------------------------------------
 # conveniences: still marshalling only
 # ---------------------------------------------------------------------------
@@ -304,3 +432,132 @@ def make_block(tokens: torch.Tensor, parent=None) -> Block:
         b.parent = ctypes.cast(arr, ctypes.POINTER(ctypes.c_int32))
         b._keep = (tokens, arr)
     return b
+
+
+class PagedCache:
+    """A paged cache over the caller's device tensors (msd.h):
+
+    k, v        [n_layers][n_pages][n_kv_heads][page_size][head_dim], bf16, or uint8 codes (8-bit pages)
+    page_table  int32 [batch_cap][max_pages]; len int32 [batch_cap]; status int32 [1]
+    k_scale, v_scale  8-bit pages: uint8 [n_layers][n_pages][n_kv_heads][page_size // 16]
+    """
+
+    def __init__(self, k, v, page_table, len, status, k_scale=None, v_scale=None):
+        fp8 = k.dtype == torch.uint8
+        _need(k.dim() == 5 and (fp8 or k.dtype == torch.bfloat16), "k: bf16 or uint8 pages [layers][pages][heads][page][dim]")
+        _typed(k, k.dtype, k.shape, "k")
+        _typed(v, k.dtype, k.shape, "v")
+        L, pages, heads, page, hd = k.shape
+        if fp8:
+            shape = (L, pages, heads, page // MSD_KV_SCALE_TOKENS)
+            _typed(k_scale, torch.uint8, shape, "k_scale")
+            _typed(v_scale, torch.uint8, shape, "v_scale")
+        else:
+            _need(k_scale is None and v_scale is None, "bf16 pages have no scales")
+        _need(page_table.dim() == 2, "page_table: [batch_cap][max_pages]")
+        batch_cap, max_pages = page_table.shape
+        _typed(page_table, torch.int32, page_table.shape, "page_table")
+        _typed(len, torch.int32, (batch_cap,), "len")
+        _typed(status, torch.int32, (1,), "status")
+        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        self.page_table, self.len, self.status = page_table, len, status
+        self.c = PagedKV(_ptr(k), _ptr(v), _ptr(k_scale), _ptr(v_scale), _ptr(page_table), _ptr(len),
+                         _ptr(status), MSD_KV_FP8 if fp8 else MSD_KV_BF16, L, pages, heads, page, hd,
+                         batch_cap, max_pages)
+        self.c._keep = (k, v, k_scale, v_scale, page_table, len, status)
+        self.c._device = k.device.index
+
+    @staticmethod
+    def allocate(n_layers: int, n_kv_heads: int, head_dim: int, n_pages: int, page_size: int,
+                 batch_cap: int, max_pages: int, fmt: str = "bf16", device="cuda") -> "PagedCache":
+        """Zeroed pages, an empty page table (every id -1) and lengths of zero; fmt "bf16" or "fp8"."""
+        _need(fmt in ("bf16", "fp8"), "fmt: bf16 or fp8")
+        dt = torch.uint8 if fmt == "fp8" else torch.bfloat16
+        kv = [torch.zeros((n_layers, n_pages, n_kv_heads, page_size, head_dim), dtype=dt, device=device)
+              for _ in range(2)]
+        sc = [torch.zeros((n_layers, n_pages, n_kv_heads, page_size // MSD_KV_SCALE_TOKENS),
+                          dtype=torch.uint8, device=device) if fmt == "fp8" else None for _ in range(2)]
+        table = torch.full((batch_cap, max_pages), -1, dtype=torch.int32, device=device)
+        return PagedCache(kv[0], kv[1], table, torch.zeros(batch_cap, dtype=torch.int32, device=device),
+                          torch.zeros(1, dtype=torch.int32, device=device), sc[0], sc[1])
+
+
+def rope(table: torch.Tensor, layout: str = "half") -> Rope:
+    """table: device fp32 [positions][rotary_dim // 2][2] of (cos, sin)."""
+    _need(layout in ROPE_LAYOUTS, "layout: half or interleaved")
+    _need(table.dim() == 3 and table.shape[2] == 2, "table: [positions][rotary_dim // 2][2]")
+    _typed(table, torch.float32, table.shape, "table")
+    r = Rope(_ptr(table), table.shape[0], 2 * table.shape[1], ROPE_LAYOUTS[layout])
+    r._keep = (table,)
+    return r
+
+
+def _strided(t: torch.Tensor, what: str):
+    """Strides of a bf16 tensor whose rows are contiguous; of an axis of one, 0."""
+    _need(t.dtype == torch.bfloat16 and t.is_cuda and t.stride(-1) == 1, f"{what}: a device bf16 tensor, last axis contiguous")
+    return [s if n > 1 else 0 for s, n in zip(t.stride()[:-1], t.shape[:-1])]
+
+
+def kv_rows(k: torch.Tensor, v: torch.Tensor, layer: int = 0, count: Optional[torch.Tensor] = None) -> KVRows:
+    """k, v: bf16 [layers][batch][rows][kv_heads][head_dim], or without the first axis for one layer; any strides
+    that are multiples of 8, the same for both. They go to the cache's layers `layer` and on."""
+    if k.dim() == 4:
+        k = k[None]
+    if v.dim() == 4:
+        v = v[None]
+    _need(k.dim() == 5 and k.shape == v.shape, "k and v: [layers][batch][rows][kv_heads][head_dim]")
+    st = _strided(k, "k")
+    _need(st == _strided(v, "v"), "k and v have the same strides")
+    if count is not None:
+        _typed(count, torch.int32, (k.shape[1],), "count")
+    r = KVRows(k.data_ptr(), v.data_ptr(), *st, layer, k.shape[0], k.shape[1], k.shape[2], _ptr(count))
+    r._keep = (k, v, count)
+    r._heads, r._device = tuple(k.shape[3:]), k.device.index
+    return r
+
+
+def paged_attn(q: torch.Tensor, out: torch.Tensor, k_new: Optional[torch.Tensor] = None,
+               v_new: Optional[torch.Tensor] = None, parent=None, count: Optional[torch.Tensor] = None,
+               rope: Optional[Rope] = None, window: int = 0, sinks: int = 0,
+               scale: Optional[float] = None) -> PagedAttn:
+    """q, out: bf16 [batch][slots][heads][head_dim]; k_new, v_new: bf16 [batch][slots][kv_heads][head_dim] of the
+    same strides; parent: host sequence or None (chain). scale: head_dim ** -0.5 unless given."""
+    _need(q.dim() == 4 and q.shape == out.shape, "q and out: [batch][slots][heads][head_dim]")
+    B, n, H, hd = q.shape
+    qs, os_ = _strided(q, "q"), _strided(out, "out")
+    _need((k_new is None) == (v_new is None), "k_new and v_new go together")
+    ns = [0, 0, 0]
+    if k_new is not None:
+        _need(k_new.dim() == 4 and k_new.shape == v_new.shape and k_new.shape[:2] == q.shape[:2] and
+              k_new.shape[3] == hd, "k_new and v_new: [batch][slots][kv_heads][head_dim]")
+        ns = _strided(k_new, "k_new")
+        _need(ns == _strided(v_new, "v_new"), "k_new and v_new have the same strides")
+    if count is not None:
+        _typed(count, torch.int32, (B,), "count")
+    arr = None
+    if parent is not None:
+        _need(len(parent) == n, "parent: one entry for each slot")
+        arr = (ctypes.c_int32 * n)(*[int(p) for p in parent])
+    a = PagedAttn(q.data_ptr(), *qs, out.data_ptr(), *os_,
+                  None if k_new is None else k_new.data_ptr(), None if v_new is None else v_new.data_ptr(), *ns,
+                  ctypes.cast(arr, ctypes.POINTER(ctypes.c_int32)) if arr is not None else None, _ptr(count),
+                  ctypes.pointer(rope) if rope is not None else None,
+                  float(hd) ** -0.5 if scale is None else float(scale), B, n, H, int(window), int(sinks))
+    a._keep = (q, out, k_new, v_new, arr, count, rope)
+    a._heads, a._device = (None if k_new is None else k_new.shape[2], hd), q.device.index
+    return a
+
+
+def sample_params(temperature: Optional[torch.Tensor] = None, top_k: Optional[torch.Tensor] = None,
+                  top_p: Optional[torch.Tensor] = None, min_p: Optional[torch.Tensor] = None) -> SampleParams:
+    """Device tensors of one value a row: fp32, top_k int32; None leaves a filter off."""
+    rows = None
+    for t, dt, what in ((temperature, torch.float32, "temperature"), (top_k, torch.int32, "top_k"),
+                        (top_p, torch.float32, "top_p"), (min_p, torch.float32, "min_p")):
+        if t is not None:
+            rows = t.numel() if rows is None else rows
+            _typed(t, dt, (rows,), what)
+    p = SampleParams(_ptr(temperature), _ptr(top_k), _ptr(top_p), _ptr(min_p))
+    p._rows = rows
+    p._keep = (temperature, top_k, top_p, min_p)
+    return p
