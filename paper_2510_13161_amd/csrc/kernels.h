@@ -328,9 +328,15 @@ struct PagedAttnArgs {
   const int32_t* count;    // [batch] or null
   float scale;
   int32_t batch, n_slots, n_heads, window, sinks;
-  Topo topo;
+  int32_t q_per_wg, groups;  // query tiles of a workgroup, workgroups that share the tiles
+  int32_t wgs;             // > 0: workgroups per kv head and group, which the sequences'
+                           // chunks share (batch <= kPagedPlanBatch); 0: one a sequence
+  float* part_o;           // [wgs][heads][groups][q_per_wg][16][hd]
+  float* part_ml;          // [wgs][heads][groups][q_per_wg][16][2]
 };
-hipError_t launch_paged_attention(bool fp8, const PagedAttnArgs& a, hipStream_t s);
+constexpr int kPagedMaxTiles = 3;     // query tiles a workgroup holds at most
+constexpr int kPagedPlanBatch = 512;  // sequences whose chunks are planned together at most
+hipError_t launch_paged_attention(bool fp8, const PagedAttnArgs& a, const Topo& topo, hipStream_t s);
 
 // ---------------------------------------------------------------------------
 // sampling

@@ -1,147 +1,92 @@
-// Attention of a block's rows over the paged cache.
-//
-// A wave owns one (sequence, query head, slot). It walks the visible keys 64 at
-// a time: each lane takes the dot product of its key with the rotated query,
-// the wave keeps a running maximum m and sum s of exp(score - m) (the output
-// rescaled when m rises), and the lanes then gather the values of the tile's
-// visible keys, each its dims.
-#include "paged.h"
+// Paged attention: dispatch, and the kernel that joins a sequence's chunks.
+#include "paged_plan.h"
 
 namespace msd {
+
+void launch_paged_bf16_64(const PagedAttnArgs& a, const Topo& topo, dim3 grid, hipStream_t s);
+void launch_paged_bf16_128(const PagedAttnArgs& a, const Topo& topo, dim3 grid, hipStream_t s);
+void launch_paged_fp8_64(const PagedAttnArgs& a, const Topo& topo, dim3 grid, hipStream_t s);
+void launch_paged_fp8_128(const PagedAttnArgs& a, const Topo& topo, dim3 grid, hipStream_t s);
+
 namespace {
 
-template <int HD, bool FP8>
-__global__ __launch_bounds__(64) void paged_attn_kernel(PagedAttnArgs a) {
-  __shared__ float qs[HD];
-  __shared__ float ps[64];
-  const int lane = threadIdx.x;
-  const int slot = blockIdx.x % a.n_slots, h = blockIdx.x / a.n_slots, b = blockIdx.y;
-  const int kvh = h / (a.n_heads / a.kv.heads);
-  const int cnt = a.count ? min(max(a.count[b], 0), a.n_slots) : a.n_slots;
-  const int64_t L = a.kv.len[b];
-  if (L < 0 || L + a.n_slots > a.kv.capacity) {
-    if (blockIdx.x == 0 && lane == 0) atomicOr(a.kv.status, 1u);
-    return;
-  }
-  if (slot >= cnt) return;
-  const int64_t P = L + a.topo.depth[slot];
-  if (lane < HD / 8) {
-    float v[8];
-    load_rotated8(a.q + b * a.q_seq + slot * a.q_row + h * a.q_head, lane, a.rope, P, v);
-    for (int i = 0; i < 8; ++i) qs[8 * lane + i] = v[i];
-  }
+// A workgroup a (sequence, kv head, query tile), a thread 8 dims of a query (half
+// of the threads idle at head dim 64).
+template <int HD>
+__global__ __launch_bounds__(256) void paged_merge_kernel(PagedAttnArgs a) {
+  __shared__ int chunk0[kPagedPlanBatch + 1];
+  const int tid = threadIdx.x;
+  int id = blockIdx.x;
+  const int kvh = id % a.kv.heads;
+  id /= a.kv.heads;
+  const int tile = id % (a.groups * a.q_per_wg);
+  const int b = id / (a.groups * a.q_per_wg);
+  const int G = a.n_heads / a.kv.heads, Qn = G * a.n_slots;
+  if (tile * 16 >= Qn) return;
+  if (tid < 64) plan_chunks(a, chunk0, false);
   __syncthreads();
-  const int page_size = 1 << a.kv.page_shift;
-  const int64_t cached = a.k_new ? L : P + 1;
-  const int64_t total = cached + (a.k_new ? slot + 1 : 0);
-  float m = -INFINITY, sum = 0.0f, o[HD / 64];
-  for (int i = 0; i < HD / 64; ++i) o[i] = 0.0f;
-  const size_t heads0 = (size_t)a.layer * a.kv.n_pages;
-  auto page_of = [&](int64_t pos) {
-    const int pg = a.kv.page_table[(size_t)b * a.kv.max_pages + (size_t)(pos >> a.kv.page_shift)];
-    return pg >= 0 && pg < a.kv.n_pages ? pg : -1;
-  };
-  for (int64_t t0 = 0; t0 < total; t0 += 64) {
-    const int64_t t = t0 + lane;
-    bool vis = false;
-    float sc = -INFINITY;
-    if (t < cached) {
-      vis = a.window <= 0 || P - t < a.window || t < a.sinks;
-      if (vis) {
-        const int pg = page_of(t);
-        if (pg < 0) {
-          atomicOr(a.kv.status, 8u);
-          vis = false;
-        } else {
-          const size_t plane = (heads0 + pg) * a.kv.heads + kvh;
-          const int off = (int)(t & (page_size - 1));
-          const size_t at = (plane * page_size + off) * HD;
-          float acc = 0.0f, f = a.scale;
-          for (int c = 0; c < HD / 8; ++c) {
-            float k[8];
-            if constexpr (FP8) {
-              const u32x2 w = *reinterpret_cast<const u32x2*>(static_cast<const uint8_t*>(a.kv.k) + at + 8 * c);
-              float k0[4], k1[4];
-              decode4(w[0], k0);
-              decode4(w[1], k1);
-              for (int i = 0; i < 4; ++i) k[i] = k0[i], k[4 + i] = k1[i];
-            } else {
-              load8(static_cast<const uint16_t*>(a.kv.k) + at + 8 * c, k);
-            }
-            for (int i = 0; i < 8; ++i) acc += qs[8 * c + i] * k[i];
-          }
-          if constexpr (FP8) f *= scale_value(a.kv.k_scale[plane * (page_size / kScaleTokens) + off / kScaleTokens]);
-          sc = acc * f;
-        }
-      }
-    } else if (t < total) {
-      const int j = (int)(t - cached);
-      const int64_t pj = L + a.topo.depth[j];
-      vis = ((a.topo.anc[slot] >> j) & 1ull) && (a.window <= 0 || P - pj < a.window || pj < a.sinks);
-      if (vis) {
-        float acc = 0.0f;
-        for (int c = 0; c < HD / 8; ++c) {
-          float k[8];
-          load_rotated8(a.k_new + b * a.new_seq + j * a.new_row + kvh * a.new_head, c, a.rope, pj, k);
-          for (int i = 0; i < 8; ++i) acc += qs[8 * c + i] * k[i];
-        }
-        sc = acc * a.scale;
-      }
+  const int u0 = chunk0[b], nch = chunk0[b + 1] - u0;
+  if (nch <= 1) return;  // none, or written by its workgroup
+  const int qloc = tid / (HD / 8), c8 = tid % (HD / 8);
+  const int qg = tile * 16 + qloc;
+  if (qloc >= 16 || qg >= Qn) return;
+  int gq, slot;
+  query_of(a, qg, gq, slot);
+  if (slot >= row_count(a, b)) return;
+  const int qgi = tile / a.q_per_wg, t = tile % a.q_per_wg;
+  float M = -INFINITY, S = 0.0f;
+  floatx4 o0 = {0.f, 0.f, 0.f, 0.f}, o1 = o0;
+  constexpr int MB = 4;  // chunks whose loads are in flight together
+  for (int c0 = 0; c0 < nch; c0 += MB) {
+    float2 ml[MB];
+    floatx4 v0[MB], v1[MB];
+#pragma unroll
+    for (int u = 0; u < MB; ++u) {
+      const int c = min(c0 + u, nch - 1);
+      const size_t row = ((((size_t)(u0 + c) * a.kv.heads + kvh) * a.groups + qgi) * a.q_per_wg + t) * 16 + qloc;
+      ml[u] = *reinterpret_cast<const float2*>(a.part_ml + 2 * row);
+      v0[u] = *reinterpret_cast<const floatx4*>(a.part_o + row * HD + 8 * c8);
+      v1[u] = *reinterpret_cast<const floatx4*>(a.part_o + row * HD + 8 * c8 + 4);
     }
-    const unsigned long long any = __ballot(vis);
-    if (!any) continue;
-    const float mt = wave_max(vis ? sc : -INFINITY);
-    const float mn = fmaxf(m, mt);
-    const float alpha = m == -INFINITY ? 0.0f : __expf(m - mn);
-    const float ref = mn == -INFINITY ? 0.0f : mn;  // every score -inf
-    const float p = vis ? expf(sc - ref) : 0.0f;
-    sum = sum * alpha + wave_sum(p);
-    m = mn;
-    for (int i = 0; i < HD / 64; ++i) o[i] *= alpha;
-    __syncthreads();
-    ps[lane] = p;
-    __syncthreads();
-    for (int k = 0; k < 64; ++k) {
-      if (!((any >> k) & 1ull)) continue;
-      const int64_t tk = t0 + k;
-      float f = ps[k];
-      if (tk < cached) {
-        const size_t plane = (heads0 + page_of(tk)) * a.kv.heads + kvh;
-        const int off = (int)(tk & (page_size - 1));
-        const size_t at = (plane * page_size + off) * HD;
-        if constexpr (FP8) f *= scale_value(a.kv.v_scale[plane * (page_size / kScaleTokens) + off / kScaleTokens]);
-        for (int i = 0; i < HD / 64; ++i) {
-          float v;
-          if constexpr (FP8) {
-            const int code = static_cast<const uint8_t*>(a.kv.v)[at + lane + 64 * i];
-            v = __builtin_amdgcn_cvt_pk_f32_fp8(code, false)[0];
-          } else {
-            v = bf2f(static_cast<const uint16_t*>(a.kv.v)[at + lane + 64 * i]);
-          }
-          o[i] += f * v;
-        }
-      } else {
-        const uint16_t* row = a.v_new + b * a.new_seq + (tk - cached) * a.new_row + kvh * a.new_head;
-        for (int i = 0; i < HD / 64; ++i) o[i] += f * bf2f(row[lane + 64 * i]);
-      }
+#pragma unroll
+    for (int u = 0; u < MB; ++u) {
+      if (c0 + u >= nch || ml[u].x == -INFINITY) continue;
+      const float Mn = fmaxf(M, ml[u].x);
+      const float fa = M == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(M - Mn);
+      const float fb = __builtin_amdgcn_exp2f(ml[u].x - Mn);
+      S = S * fa + ml[u].y * fb;
+      o0 = o0 * fa + v0[u] * fb;
+      o1 = o1 * fa + v1[u] * fb;
+      M = Mn;
     }
   }
-  uint16_t* dst = a.out + b * a.out_seq + slot * a.out_row + h * a.out_head;
-  const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-  for (int i = 0; i < HD / 64; ++i) dst[lane + 64 * i] = f2bf(o[i] * inv);
+  const float inv = S != 0.0f ? 1.0f / S : 0.0f;
+  o0 *= inv;
+  o1 *= inv;
+  const u32x4 y = {pack_bf16x2(o0[0], o0[1]), pack_bf16x2(o0[2], o0[3]), pack_bf16x2(o1[0], o1[1]),
+                   pack_bf16x2(o1[2], o1[3])};
+  *reinterpret_cast<u32x4*>(a.out + b * a.out_seq + slot * a.out_row + (kvh * G + gq) * a.out_head + 8 * c8) = y;
 }
 
 }  // namespace
 
-hipError_t launch_paged_attention(bool fp8, const PagedAttnArgs& a, hipStream_t s) {
-  const dim3 grid(a.n_heads * a.n_slots, a.batch), block(64);
+hipError_t launch_paged_attention(bool fp8, const PagedAttnArgs& a, const Topo& topo, hipStream_t s) {
+  const int64_t wgs = (int64_t)(a.wgs > 0 ? a.wgs : a.batch) * a.kv.heads * a.groups;
+  if (wgs > 0x7FFFFFFF / 256 || a.q_per_wg < 1 || a.q_per_wg > kPagedMaxTiles || (a.wgs > 0 && a.batch > kPagedPlanBatch))
+    return hipErrorInvalidValue;
+  const dim3 grid((uint32_t)wgs);
   if (a.kv.head_dim == 128) {
-    if (fp8) hipLaunchKernelGGL((paged_attn_kernel<128, true>), grid, block, 0, s, a);
-    else hipLaunchKernelGGL((paged_attn_kernel<128, false>), grid, block, 0, s, a);
+    if (fp8) launch_paged_fp8_128(a, topo, grid, s);
+    else launch_paged_bf16_128(a, topo, grid, s);
   } else {
-    if (fp8) hipLaunchKernelGGL((paged_attn_kernel<64, true>), grid, block, 0, s, a);
-    else hipLaunchKernelGGL((paged_attn_kernel<64, false>), grid, block, 0, s, a);
+    if (fp8) launch_paged_fp8_64(a, topo, grid, s);
+    else launch_paged_bf16_64(a, topo, grid, s);
   }
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || a.wgs == 0) return e;
+  const dim3 merge((uint32_t)((int64_t)a.batch * a.kv.heads * a.groups * a.q_per_wg));
+  if (a.kv.head_dim == 128) hipLaunchKernelGGL(paged_merge_kernel<128>, merge, dim3(256), 0, s, a);
+  else hipLaunchKernelGGL(paged_merge_kernel<64>, merge, dim3(256), 0, s, a);
   return hipGetLastError();
 }
 

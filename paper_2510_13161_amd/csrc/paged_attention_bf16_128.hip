@@ -1,0 +1,8 @@
+// The paged attention kernels of head dim 128 over bf16 pages (a source of their own: they build side by side).
+#include "paged_attention.h"
+
+namespace msd {
+void launch_paged_bf16_128(const PagedAttnArgs& a, const Topo& topo, dim3 grid, hipStream_t s) {
+  launch_tiles<128, false>(a, topo, grid, s);
+}
+}  // namespace msd

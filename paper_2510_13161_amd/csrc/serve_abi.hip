@@ -1,6 +1,7 @@
 // C ABI of the serving operators (include/msd.h): the paged cache's append,
 // commit and attention, and sampling. Argument checks and launches; every call
 // is asynchronous on the caller's stream and allocates nothing.
+#include <algorithm>
 #include <cmath>
 
 #include "serve.h"
@@ -84,6 +85,31 @@ msd_status fill_append(const msd_paged_kv* kv, const msd_kv_rows* rows, const ms
   return MSD_OK;
 }
 
+// Launch shape of an attention call. Query tiles: as few groups as hold them,
+// evenly (each group reads the keys again). Workgroups: where the sequences alone
+// fill fewer than kPagedWgs of them and a sequence can have more blocks than two
+// for each wave, chunks are planned on the device over kPagedWgs workgroups and
+// joined by a second kernel.
+constexpr int64_t kPagedWgs = 256;
+constexpr int64_t kPagedAlone = 8;  // 64-key blocks that one workgroup takes without a split
+struct PagedShape {
+  int q_per_wg, groups, wgs;
+};
+PagedShape paged_shape(int32_t batch, int32_t n_slots, int32_t n_heads, int32_t heads, int64_t blocks) {
+  const int tiles = (n_heads / heads * n_slots + 15) / 16;
+  PagedShape s;
+  s.groups = (tiles + kPagedMaxTiles - 1) / kPagedMaxTiles;
+  s.q_per_wg = (tiles + s.groups - 1) / s.groups;
+  const int64_t share = kPagedWgs / ((int64_t)heads * s.groups);
+  s.wgs = blocks <= kPagedAlone || share <= batch || batch > kPagedPlanBatch
+              ? 0
+              : (int)std::min<int64_t>(share, batch * ((blocks + 3) / 4));
+  return s;
+}
+size_t paged_partials(const PagedShape& s, int32_t heads, int32_t hd) {
+  return (size_t)s.wgs * heads * s.groups * s.q_per_wg * 16 * (hd + 2) * sizeof(float);
+}
+
 }  // namespace
 
 extern "C" {
@@ -114,8 +140,13 @@ msd_status msd_paged_commit(const msd_paged_kv* kv, const msd_kv_rows* rows, con
 
 size_t msd_paged_attention_workspace_bytes(const msd_paged_kv* kv, int32_t batch, int32_t n_slots,
                                            int32_t n_heads) {
-  if (!kv || batch < 1 || n_slots < 1 || n_heads < 1) return 0;
-  return 16;
+  if (!kv || batch < 1 || n_slots < 1 || n_heads < 1 || kv->n_kv_heads < 1) return 0;
+  // The most that any smaller call uses: shares of kPagedWgs workgroups of at most
+  // kPagedMaxTiles tiles, of the call's own tiles at most, and at least one
+  // workgroup for each kv head and group.
+  const size_t tiles = ((size_t)((n_heads + kv->n_kv_heads - 1) / kv->n_kv_heads) * n_slots + 15) / 16;
+  const size_t wgs = (size_t)kPagedWgs;
+  return wgs * std::min<size_t>(tiles, kPagedMaxTiles) * 16 * (kv->head_dim + 2) * sizeof(float) + 16;
 }
 
 msd_status msd_paged_attention(const msd_paged_kv* kv, int32_t layer, const msd_paged_attn* at, void* ws,
@@ -143,13 +174,27 @@ msd_status msd_paged_attention(const msd_paged_kv* kv, int32_t layer, const msd_
   if (at->window < 0 || at->sinks < 0) return report(MSD_ERR_INVALID_ARG, "window and sinks must be >= 0");
   if (!at->k_new && at->parent) return report(MSD_ERR_UNSUPPORTED, "a tree needs its keys in k_new and v_new");
   if (a.kv.capacity < at->n_slots) return report(MSD_ERR_CAPACITY, "max_pages * page_size below n_slots");
-  if (!topo_from(at->parent, at->n_slots, &a.topo))
+  Topo topo;
+  if (!topo_from(at->parent, at->n_slots, &topo))
     return report(MSD_ERR_SHAPE, "parent[0] must be -1 and parent[i] lie in [0, i)");
   st = check_rope(at->rope, a.kv, &a.rope);
   if (st != MSD_OK) return st;
   if (!ws || !aligned16(ws) ||
       ws_bytes < msd_paged_attention_workspace_bytes(kv, at->batch, at->n_slots, at->n_heads))
     return report(MSD_ERR_WORKSPACE, "workspace NULL, unaligned or too small");
+  // blocks that a sequence can have: of its whole capacity, or of the sinks and the window
+  int64_t blocks = (a.kv.capacity + 63) / 64;
+  if (at->window > 0)
+    blocks = std::min(blocks, ((int64_t)at->sinks + 63) / 64 + ((int64_t)at->window + at->n_slots + 62) / 64 + 1);
+  const PagedShape sh = paged_shape(at->batch, at->n_slots, at->n_heads, kv->n_kv_heads, blocks + (at->k_new ? 1 : 0));
+  a.q_per_wg = sh.q_per_wg;
+  a.groups = sh.groups;
+  a.wgs = sh.wgs;
+  const size_t rows = (size_t)sh.wgs * kv->n_kv_heads * sh.groups * sh.q_per_wg * 16;
+  a.part_o = static_cast<float*>(ws);
+  a.part_ml = a.part_o + rows * kv->head_dim;
+  if (paged_partials(sh, kv->n_kv_heads, kv->head_dim) > ws_bytes)
+    return report(MSD_ERR_WORKSPACE, "workspace too small");
   a.layer = layer;
   a.q = static_cast<const uint16_t*>(at->q);
   a.q_seq = at->q_seq;
@@ -171,7 +216,7 @@ msd_status msd_paged_attention(const msd_paged_kv* kv, int32_t layer, const msd_
   a.n_heads = at->n_heads;
   a.window = at->window;
   a.sinks = at->sinks;
-  return hip_fail(launch_paged_attention(kv->format == MSD_KV_FP8, a, stream));
+  return hip_fail(launch_paged_attention(kv->format == MSD_KV_FP8, a, topo, stream));
 }
 
 size_t msd_sample_workspace_bytes(int32_t rows, int32_t vocab) {
