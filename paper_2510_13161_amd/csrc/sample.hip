@@ -1,258 +1,597 @@
 // Sampling under temperature, top-k, top-p and min-p from given uniforms.
 //
-// Tokens are ranked by (logit descending, id ascending); every filter keeps a
-// prefix of that order, so the kept set is the ids with (z, id) at or above one
-// threshold. Masses exp((z - max) / T) are fp64 values rounded to multiples of
-// 2^-43: integer sums, the same in any order, so that histograms may be
-// filled with atomics and a run repeats bit for bit (2^20 tokens of mass one
-// fill 2^63). A workgroup owns a row. The threshold is found digit by digit of the
-// ordered fp32 bits (11, 11 and 10): a histogram of counts and masses of the
-// tokens that share the digits so far, then the digit at which the running
-// count reaches top_k, or the running mass top_p of the total. Equal logits at
-// the threshold are cut in id order.
+// Tokens are ranked by (logit descending, id ascending), one 64-bit key; every
+// filter keeps a prefix of that order, so the kept set is the keys at or above one
+// threshold. Masses 2^t, t = (z - max) log2(e) / T, are fp64 values rounded to
+// multiples of 2^-43: integer sums, the same in any order, so that
+// histograms may be filled with atomics and a run repeats bit for bit (2^20
+// tokens of mass one fill 2^63).
+//
+//  1 top    a workgroup a chunk of 8192 logits: its largest.
+//  2 tally  the chunk again (held in registers, 16 a thread): masses, and for
+//           filtered rows a histogram of counts and masses over half octaves of 2^t
+//           down to 2^-64, and the keys of the chunk's highest half octaves,
+//           as many as fit 512 keys.
+//  3 draw   a workgroup a row: the histograms added up and scanned from the top give
+//           the half octave in which top-k cuts, then (of what that
+//           leaves) top-p. Where the chunks' lists reach down to it, the cut is
+//           found among them: the keys of that half octave are ranked by counting,
+//           their masses scanned in that order. Else (flat laws, whose kept
+//           sets are a large part of the vocabulary) digit by digit over
+//           the row. The draw: masses of 512-id segments, the segment, the id.
+//           Unfiltered rows take the chunk from the chunks' masses.
 #include "sample.h"
 
 namespace msd {
 namespace {
 
-constexpr int kThreads = 1024;
-constexpr int kBins = 2048;
+constexpr int kChunk = 8192, kTally = 512, kEach = kChunk / kTally;
+constexpr int kBins = 128;        // half octaves; the last takes all below 2^-63.5
+constexpr int kList = 512;        // keys of a chunk's list
+constexpr int kDraw = 1024;       // threads of the draw
+constexpr int kCands = 8192;      // keys that the draw holds
+constexpr int kSeg = 512;         // ids of a segment
+constexpr int kSegs = (1 << 20) / kSeg;
+constexpr int kDigit = 2048;      // digit values of the search over a row
+
+struct Chunk {
+  uint32_t n_list;   // keys in its list
+  int32_t list_bin;  // the list holds all its tokens of bins <= list_bin
+  uint64_t mass;     // of all its tokens
+  uint64_t tokens;   // above -inf
+};
+
+// Workspace of a row: [chunks] top keys, Chunk records, counts [kBins], masses
+// [kBins], lists [kList].
+struct Work {
+  uint32_t* top;
+  Chunk* head;
+  uint32_t* cnt;
+  uint64_t* mass;
+  uint64_t* list;
+};
+__host__ __device__ inline int chunks_of(int vocab) { return (vocab + kChunk - 1) / kChunk; }
+__host__ __device__ inline size_t row_bytes(int C) {
+  const size_t b = (size_t)C * (kList * 8 + kBins * 12 + sizeof(Chunk) + 4);
+  return (b + 15) / 16 * 16;
+}
+__device__ __forceinline__ Work work_of(const SampleArgs& a, int row, int C) {
+  char* p = static_cast<char*>(a.ws) + row_bytes(C) * row;
+  Work w;
+  w.list = reinterpret_cast<uint64_t*>(p);
+  w.mass = w.list + (size_t)C * kList;
+  w.head = reinterpret_cast<Chunk*>(w.mass + (size_t)C * kBins);
+  w.cnt = reinterpret_cast<uint32_t*>(w.head + C);
+  w.top = w.cnt + (size_t)C * kBins;
+  return w;
+}
+
+__device__ __forceinline__ int bin_of(double t) { return (int)fmin(-2.0 * t, (double)(kBins - 1)); }
+
+__device__ __forceinline__ uint32_t wave_max_u32(uint32_t v) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) v = max(v, (uint32_t)__shfl_xor((int)v, o));
+  return v;
+}
+__device__ __forceinline__ uint64_t wave_sum_u64(uint64_t v) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o);
+  return v;
+}
+__device__ __forceinline__ uint64_t wave_scan_u64(uint64_t v) {  // inclusive
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const uint64_t y = __shfl_up(v, o);
+    if (lane >= o) v += y;
+  }
+  return v;
+}
+
+__global__ __launch_bounds__(kTally) void top_kernel(SampleArgs a) {
+  __shared__ uint32_t red[kTally / 64];
+  const int c = blockIdx.x, row = blockIdx.y, tid = threadIdx.x;
+  const float* z = a.logits + (int64_t)row * a.row_stride;
+  uint32_t top = 0;
+#pragma unroll
+  for (int j = 0; j < kEach; ++j) {
+    const int i = c * kChunk + j * kTally + tid;
+    if (i < a.vocab) top = max(top, ordered_bits(clean(z[i])));
+  }
+  top = wave_max_u32(top);
+  if ((tid & 63) == 0) red[tid >> 6] = top;
+  __syncthreads();
+  if (tid == 0) {
+    for (int w = 1; w < kTally / 64; ++w) top = max(top, red[w]);
+    work_of(a, row, gridDim.x).top[c] = top;
+  }
+}
+
+__global__ __launch_bounds__(kTally) void tally_kernel(SampleArgs a) {
+  __shared__ uint32_t cnt[kBins];
+  __shared__ unsigned long long mass[kBins];
+  __shared__ uint64_t red[kTally / 64];
+  __shared__ uint32_t red_n[kTally / 64];
+  __shared__ uint32_t n_list;
+  __shared__ int list_bin;
+  const int C = gridDim.x, c = blockIdx.x, row = blockIdx.y, tid = threadIdx.x;
+  const Work w = work_of(a, row, C);
+  const float* z = a.logits + (int64_t)row * a.row_stride;
+  float v[kEach];
+#pragma unroll
+  for (int j = 0; j < kEach; ++j) {
+    const int i = c * kChunk + j * kTally + tid;
+    v[j] = i < a.vocab ? clean(z[i]) : -INFINITY;
+  }
+  uint32_t top = 0;
+  for (int i = tid & 63; i < C; i += 64) top = max(top, w.top[i]);
+  top = wave_max_u32(top);
+  if (top <= kDead) return;  // no token
+  const float ref = from_ordered_bits(top);
+  const Request q = request_of(a, row);
+  const bool filtered = q.filtered();
+  if (tid < kBins) cnt[tid] = 0, mass[tid] = 0;
+  if (tid == 0) n_list = 0;
+  __syncthreads();
+  uint64_t sum = 0;
+  uint32_t tokens = 0;
+  uint32_t low = 0;  // tokens of the last bin, which most tokens of cold laws share
+#pragma unroll
+  for (int j = 0; j < kEach; ++j) {
+    if (v[j] == -INFINITY) continue;
+    const double t = exponent_of(v[j], ref, q.c);
+    const uint64_t m = mass_of(t);
+    sum += m;
+    ++tokens;
+    if (!filtered) continue;
+    const int b = bin_of(t);
+    if (b == kBins - 1) {
+      ++low;
+      continue;
+    }
+    atomicAdd(&cnt[b], 1u);
+    if (m) atomicAdd(&mass[b], (unsigned long long)m);
+  }
+  sum = wave_sum_u64(sum);
+  tokens = (uint32_t)wave_sum_u64(tokens);
+  if (low) atomicAdd(&cnt[kBins - 1], low);
+  if ((tid & 63) == 0) red[tid >> 6] = sum, red_n[tid >> 6] = tokens;
+  __syncthreads();
+  if (tid < 64) {
+    // the deepest bin down to which the chunk's tokens fit its list
+    const uint32_t c0 = cnt[2 * tid], c1 = cnt[2 * tid + 1];
+    const uint64_t x = wave_scan_u64(c0 + c1);
+    const int fit = (x - c1 <= kList) + (x <= kList);  // prefix counts: of this lane's two bins
+    int f = fit;
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) f += __shfl_xor(f, o);
+    if (tid == 0) {
+      list_bin = f - 1;
+      for (int i = 1; i < kTally / 64; ++i) red[0] += red[i], red_n[0] += red_n[i];
+    }
+  }
+  __syncthreads();
+  if (filtered) {
+    const int lb = list_bin;
+#pragma unroll
+    for (int j = 0; j < kEach; ++j) {
+      if (v[j] == -INFINITY || bin_of(exponent_of(v[j], ref, q.c)) > lb) continue;
+      w.list[(size_t)c * kList + atomicAdd(&n_list, 1u)] = rank_key(v[j], c * kChunk + j * kTally + tid);
+    }
+    if (tid < kBins) {
+      w.cnt[(size_t)c * kBins + tid] = cnt[tid];
+      w.mass[(size_t)c * kBins + tid] = mass[tid];
+    }
+    __syncthreads();
+  }
+  if (tid == 0) w.head[c] = Chunk{n_list, list_bin, red[0], red_n[0]};
+}
 
 struct Shared {
+  uint64_t cand[kCands];       // keys; in the search over a row: digit masses
+  uint64_t seg[kSegs];         // segment masses; before: masses by rank
+  uint64_t red[kDraw / 64 + 1];
+  uint64_t mass[kBins];        // tokens of the bins above, then of the bin
   uint32_t cnt[kBins];
-  uint64_t mass[kBins];
-  uint64_t wave[kThreads / 64];
-  uint32_t wave_max[kThreads / 64];
-  uint64_t above_mass;
-  uint64_t mass_sel;
-  uint32_t above_cnt, cnt_sel, bin, id;
+  uint64_t above_mass, key, want_bits;
+  uint32_t above, n, m, pick;
+  int min_list;
 };
+static_assert(kCands * 8 >= kDigit * 12, "digit histograms fit the key list");
+
+// inclusive block scan over kDraw threads; total in sh.red[kDraw / 64]
+__device__ __forceinline__ uint64_t block_scan(Shared& sh, uint64_t v) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const uint64_t x = wave_scan_u64(v);
+  __syncthreads();
+  if (lane == 63) sh.red[wave] = x;
+  __syncthreads();
+  if (wave == 0) {
+    const uint64_t y = lane < kDraw / 64 ? sh.red[lane] : 0;
+    const uint64_t s = wave_scan_u64(y);
+    if (lane < kDraw / 64) sh.red[lane] = s - y;
+    if (lane == kDraw / 64 - 1) sh.red[kDraw / 64] = s;
+  }
+  __syncthreads();
+  return x + sh.red[wave];
+}
 
 struct Row {
   const float* z;
-  int V, tid;
-  double inv_ref, T;  // largest logit, temperature
+  int V;
+  float ref;   // the largest logit
+  uint32_t top;
+  Request q;
+  uint64_t threshold;  // smallest kept key
+  __device__ uint64_t weight(int i, bool& kept) const {
+    const float x = clean(z[i]);
+    kept = false;
+    if (x == -INFINITY || rank_key(x, i) < threshold) return 0;
+    const double t = exponent_of(x, ref, q.c);
+    if (q.min_p > 0.0 && x != ref && exp2_64(t, 0) < q.min_p) return 0;
+    kept = true;
+    return mass_of(t);
+  }
 };
 
-__device__ uint64_t block_sum(Shared& sh, uint64_t v) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o);
-  __syncthreads();
-  if ((threadIdx.x & 63) == 0) sh.wave[threadIdx.x >> 6] = v;
-  __syncthreads();
-  uint64_t t = 0;
-  for (int w = 0; w < kThreads / 64; ++w) t += sh.wave[w];
-  return t;
-}
-
-// Tokens whose ordered bits lie at or above lo ... are kept down to a cut: by
-// count (the n-th) or by mass (before < want). Finds the key of the last kept
-// logit, the number of kept tokens with exactly that logit, and the count and
-// mass of all tokens above it.
-struct Cut {
-  uint32_t key;        // ordered bits of the threshold logit
-  uint32_t ties;       // kept tokens with that logit
-  uint32_t above;      // tokens above it
-  uint64_t above_mass;
-};
-
+// The key at which the kept prefix ends, searched digit by digit (11, 11 and 10
+// bits of the ordered logit) over the row's tokens with key >= floor: the n-th
+// (by count), or the last whose preceding mass is below `want`. Equal logits are
+// cut in id order.
 template <bool BY_MASS>
-__device__ Cut find_cut(Shared& sh, const Row& r, uint64_t n, double want, uint32_t floor_key) {
-  uint32_t prefix = 0, above = 0;
-  uint64_t above_mass = 0;
+__device__ uint64_t search_row(Shared& sh, const Row& r, uint64_t n, double want, uint64_t floor) {
+  uint64_t* mass = sh.cand;
+  uint32_t* cnt = reinterpret_cast<uint32_t*>(mass + kDigit);
+  const int tid = threadIdx.x;
+  uint32_t prefix = 0;
+  uint64_t above = 0, above_mass = 0;
+  uint32_t equal = 0;
   for (int level = 0; level < 3; ++level) {
     const int shift = level == 0 ? 21 : (level == 1 ? 10 : 0);
     const int bits = level == 2 ? 10 : 11;
-    for (int i = r.tid; i < kBins; i += kThreads) sh.cnt[i] = 0, sh.mass[i] = 0;
     __syncthreads();
-    for (int i = r.tid; i < r.V; i += kThreads) {
+    for (int i = tid; i < kDigit; i += kDraw) cnt[i] = 0, mass[i] = 0;
+    __syncthreads();
+    for (int i = tid; i < r.V; i += kDraw) {
       const float z = clean(r.z[i]);
       const uint32_t k = ordered_bits(z);
-      if (k <= kDead || (level && (k >> (shift + bits)) != prefix) || k < floor_key) continue;
+      if (k <= kDead || (level && (k >> (shift + bits)) != prefix) || rank_key(z, i) < floor) continue;
       const uint32_t d = (k >> shift) & ((1u << bits) - 1);
-      atomicAdd(&sh.cnt[d], 1u);
-      if (BY_MASS) atomicAdd((unsigned long long*)&sh.mass[d], (unsigned long long)mass_of(z, r.inv_ref, r.T));
-    }
-    __syncthreads();
-    if (r.tid == 0) {
-      int d = (1 << bits) - 1, last = d;
-      uint32_t c = above, c_last = above;
-      uint64_t m = above_mass, m_last = above_mass;
-      bool any = false;
-      for (; d >= 0; --d) {
-        if (!sh.cnt[d]) continue;
-        const bool inside = BY_MASS ? (double)m < want || c == 0 : c < n;
-        if (!inside) break;
-        any = true;
-        last = d, c_last = c, m_last = m;
-        c += sh.cnt[d];
-        m += sh.mass[d];
+      atomicAdd(&cnt[d], 1u);
+      if (BY_MASS) {
+        const uint64_t m = mass_of(exponent_of(z, r.ref, r.q.c));
+        if (m) atomicAdd((unsigned long long*)&mass[d], (unsigned long long)m);
       }
-      sh.bin = any ? last : 0;
-      sh.above_cnt = c_last;
-      sh.above_mass = m_last;
     }
     __syncthreads();
-    prefix = (prefix << bits) | sh.bin;
-    above = sh.above_cnt;
+    // scanned from the largest digit: thread t holds digits D - 1 - 2 t and D - 2 - 2 t
+    const int D = 1 << bits;
+    const int d0 = D - 1 - 2 * tid, d1 = d0 - 1;
+    const uint64_t c0 = d0 >= 0 ? cnt[d0] : 0, c1 = d1 >= 0 ? cnt[d1] : 0;
+    const uint64_t m0 = d0 >= 0 ? mass[d0] : 0, m1 = d1 >= 0 ? mass[d1] : 0;
+    const uint64_t cs = above + block_scan(sh, c0 + c1) - c0 - c1;
+    const uint64_t ms = BY_MASS ? above_mass + block_scan(sh, m0 + m1) - m0 - m1 : 0;
+    // the last non-empty digit that starts inside
+    auto inside = [&](uint64_t cb, uint64_t mb) { return BY_MASS ? (cb == 0 || (double)mb < want) : cb < n; };
+    int last = -1;
+    if (c0 && inside(cs, ms)) last = 2 * tid;
+    if (c1 && inside(cs + c0, ms + m0)) last = 2 * tid + 1;
+    if (tid == 0) sh.m = 0;
+    __syncthreads();
+    if (last >= 0) atomicMax(&sh.m, (uint32_t)last);
+    __syncthreads();
+    if (last >= 0 && sh.m == (uint32_t)last) {
+      sh.pick = D - 1 - last;
+      sh.key = cs + (last & 1 ? c0 : 0);
+      sh.above_mass = ms + (last & 1 ? m0 : 0);
+      sh.n = (uint32_t)(last & 1 ? c1 : c0);
+    }
+    __syncthreads();
+    prefix = (prefix << bits) | sh.pick;
+    above = sh.key;
     above_mass = sh.above_mass;
-    __syncthreads();
+    equal = sh.n;
   }
-  Cut c{prefix, 0, above, above_mass};
-  // all with the threshold's logit: the last level's bin is one key
-  const uint32_t equal = sh.cnt[prefix & 1023];
+  // of the `equal` tokens with this logit, the first t ids
+  uint32_t t = equal;
   if (BY_MASS) {
-    const uint64_t one = mass_of(from_ordered_bits(prefix), r.inv_ref, r.T);
-    uint32_t lo = 0, hi = equal;  // smallest t >= 1 with above + t * one >= want
-    while (lo + 1 < hi) {
-      const uint32_t mid = (lo + hi) / 2;
+    const uint64_t one = mass_of(exponent_of(from_ordered_bits(prefix), r.ref, r.q.c));
+    uint32_t lo = 0;  // smallest t >= 1 with above_mass + t * one >= want, at most equal
+    while (lo + 1 < t) {
+      const uint32_t mid = (lo + t) / 2;
       if ((double)(above_mass + mid * one) < want) lo = mid;
-      else hi = mid;
+      else t = mid;
     }
-    c.ties = hi;
-  } else {
-    c.ties = (uint32_t)(n - above < equal ? n - above : equal);
+  } else if (n - above < equal) {
+    t = (uint32_t)(n - above);
+  }
+  if (t == equal) return (uint64_t)prefix << 32;  // all of them
+  // the t-th id: equal logits counted by blocks of kDraw ids
+  uint32_t seen = 0;
+  for (int i0 = 0; i0 < r.V; i0 += kDraw) {
+    const int i = i0 + tid;
+    const bool is = i < r.V && ordered_bits(clean(r.z[i])) == prefix;
+    const uint64_t x = block_scan(sh, is ? 1 : 0);
+    if (is && seen + x == t) sh.key = rank_key(from_ordered_bits(prefix), i);
+    seen += (uint32_t)sh.red[kDraw / 64];
+    if (seen >= t) break;
   }
   __syncthreads();
-  return c;
+  return sh.key;
 }
 
-// mass of the tokens above key, and the id of the t-th token with that key
-__device__ uint32_t tie_id(Shared& sh, const Row& r, uint32_t key, uint32_t t) {
-  // contiguous chunk of ids per thread, counted, prefixed, scanned
-  const int per = (r.V + kThreads - 1) / kThreads;
-  const int i0 = min(r.tid * per, r.V), i1 = min(i0 + per, r.V);
-  uint32_t mine = 0;
-  for (int i = i0; i < i1; ++i) mine += ordered_bits(clean(r.z[i])) == key;
+// The same among the candidate keys: those of bin `bin`, at most kDraw, ranked by
+// counting; `above` tokens and `above_mass` lie in the bins before.
+template <bool BY_MASS>
+__device__ uint64_t search_bin(Shared& sh, const Row& r, uint32_t N, int bin, uint64_t n, double want, uint64_t above,
+                               uint64_t above_mass, uint64_t floor, uint64_t* kept_mass) {
+  const int tid = threadIdx.x;
+  uint64_t* mine = sh.seg;  // keys of the bin
   __syncthreads();
-  sh.cnt[r.tid] = mine;
+  if (tid == 0) sh.m = 0;
   __syncthreads();
-  if (r.tid == 0) {
-    uint32_t c = 0;
-    for (int i = 0; i < kThreads; ++i) {
-      const uint32_t x = sh.cnt[i];
-      sh.cnt[i] = c;
-      c += x;
-    }
-    sh.id = r.V - 1;
+  for (uint32_t i = tid; i < N; i += kDraw) {
+    const uint64_t k = sh.cand[i];
+    if (k >= floor && bin_of(exponent_of(key_val(k), r.ref, r.q.c)) == bin) mine[atomicAdd(&sh.m, 1u)] = k;
   }
   __syncthreads();
-  uint32_t c = sh.cnt[r.tid];
-  if (c < t && c + mine >= t)
-    for (int i = i0; i < i1; ++i)
-      if (ordered_bits(clean(r.z[i])) == key && ++c == t) sh.id = i;
+  const uint32_t m = sh.m;
+  const uint64_t key = tid < (int)m ? mine[tid] : 0;
+  uint32_t rank = 0;
+  for (uint32_t i = 0; i < m; ++i) rank += mine[i] > key;
   __syncthreads();
-  const uint32_t id = sh.id;
+  uint64_t* by_rank = sh.seg;               // masses
+  uint64_t* key_by_rank = sh.seg + kDraw;
+  if (tid < (int)m) {
+    by_rank[rank] = mass_of(exponent_of(key_val(key), r.ref, r.q.c));
+    key_by_rank[rank] = key;
+  }
   __syncthreads();
-  return id;
+  const uint64_t w = tid < (int)m ? by_rank[tid] : 0;
+  const uint64_t x = above_mass + block_scan(sh, w);  // mass through rank tid
+  bool in;
+  if (BY_MASS) in = tid < (int)m && ((double)(x - w) < want || above + tid == 0);
+  else in = tid < (int)m && above + tid < n;
+  // ranks inside are a prefix: the last of them
+  if (in && (tid + 1 == (int)m || !(BY_MASS ? (double)x < want : above + tid + 1 < n))) {
+    sh.key = key_by_rank[tid];
+    sh.above_mass = x;
+  }
+  __syncthreads();
+  *kept_mass = sh.above_mass;
+  return sh.key;
 }
+static_assert(kSegs >= 2 * kDraw, "ranks and their keys fit the segment masses");
 
-__global__ __launch_bounds__(kThreads) void sample_kernel(SampleArgs a) {
+__global__ __launch_bounds__(kDraw) void draw_kernel(SampleArgs a, int C) {
   __shared__ Shared sh;
-  const int row = blockIdx.x;
+  const int row = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const Work w = work_of(a, row, C);
   Row r;
   r.z = a.logits + (int64_t)row * a.row_stride;
   r.V = a.vocab;
-  r.tid = threadIdx.x;
-  const Params p = params_of(a, row);
+  r.q = request_of(a, row);
   uint32_t top = 0;
-  for (int i = r.tid; i < r.V; i += kThreads) top = max(top, ordered_bits(clean(r.z[i])));
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, o));
-  if ((r.tid & 63) == 0) sh.wave_max[r.tid >> 6] = top;
-  __syncthreads();
-  for (int w = 0; w < kThreads / 64; ++w) top = max(top, sh.wave_max[w]);
-  if (top <= kDead) {
-    if (r.tid == 0) {
+  for (int i = lane; i < C; i += 64) top = max(top, w.top[i]);
+  r.top = wave_max_u32(top);
+  if (r.top <= kDead) {
+    if (tid == 0) {
       a.tok[row] = -1;
       if (a.logp) a.logp[row] = -INFINITY;
       if (a.kept) a.kept[row] = 0;
     }
     return;
   }
-  r.T = p.T;
-  r.inv_ref = (double)from_ordered_bits(top);
-  // threshold: (key, id of the last kept tie)
-  uint32_t key = kDead + 1, last_id = 0xFFFFFFFFu;
-  uint64_t total = 0;
-  if (p.k < (uint32_t)r.V) {
-    const Cut c = find_cut<false>(sh, r, p.k, 0.0, 0);
-    key = c.key;
-    last_id = tie_id(sh, r, c.key, c.ties);
-  }
-  auto kept = [&](int i, float z, uint32_t k) {
-    return k > key || (k == key && (uint32_t)i <= last_id);
-  };
-  if (p.p < 1.0) {
-    uint64_t m = 0;
-    for (int i = r.tid; i < r.V; i += kThreads) {
-      const float z = clean(r.z[i]);
-      const uint32_t k = ordered_bits(z);
-      if (k > kDead && kept(i, z, k)) m += mass_of(z, r.inv_ref, r.T);
-    }
-    total = block_sum(sh, m);
-    const Cut c = find_cut<true>(sh, r, 0, p.p * (double)total, key);
-    const uint32_t id = tie_id(sh, r, c.key, c.ties);
-    last_id = c.key == key ? min(id, last_id) : id;
-    key = c.key;
-  }
-  // kept mass of each thread's contiguous ids, then the draw
-  const int per = (r.V + kThreads - 1) / kThreads;
-  const int i0 = min(r.tid * per, r.V), i1 = min(i0 + per, r.V);
-  uint64_t m = 0;
-  uint32_t n = 0;
-  auto weight = [&](int i, uint32_t& count) -> uint64_t {
-    const float z = clean(r.z[i]);
-    const uint32_t k = ordered_bits(z);
-    if (k <= kDead || !kept(i, z, k) || (k != top && !over_min(z, r.inv_ref, r.T, p.min_p))) return 0;
-    ++count;
-    return mass_of(z, r.inv_ref, r.T);
-  };
-  for (int i = i0; i < i1; ++i) m += weight(i, n);
-  total = block_sum(sh, m);
-  const uint32_t n_kept = (uint32_t)block_sum(sh, n);
-  sh.mass[r.tid] = m;
-  __syncthreads();
-  if (r.tid == 0) {
-    const double want = p.u * (double)total;
-    uint64_t c = 0;
-    int w = 0, found = -1;
-    uint64_t before = 0;
-    for (; w < kThreads; ++w) {
-      if (sh.mass[w] && (double)(c + sh.mass[w]) > want) {
-        found = w, before = c;
-        break;
+  r.ref = from_ordered_bits(r.top);
+  r.threshold = 0;
+  const bool filtered = r.q.filtered();
+  uint32_t n_kept = 0;
+  const int n_seg = (r.V + kSeg - 1) / kSeg;
+  int first_seg = 0, last_seg = n_seg;  // segments whose masses are in sh.seg
+  uint64_t total = 0, before = 0;       // all kept mass; that of the segments before first_seg
+  bool from_list = false;
+  uint32_t N = 0;
+
+  if (filtered) {
+    if (tid < kBins) sh.cnt[tid] = 0, sh.mass[tid] = 0;
+    if (tid == 0) sh.min_list = kBins, sh.n = 0;
+    __syncthreads();
+    {
+      uint32_t n = 0;
+      uint64_t m = 0;
+      const int b = tid % kBins;
+      for (int c = tid / kBins; c < C; c += kDraw / kBins) {
+        n += w.cnt[(size_t)c * kBins + b];
+        m += w.mass[(size_t)c * kBins + b];
       }
-      if (sh.mass[w]) found = w, before = c;
-      c += sh.mass[w];
+      if (n) atomicAdd(&sh.cnt[b], n);
+      if (m) atomicAdd((unsigned long long*)&sh.mass[b], (unsigned long long)m);
+      if (tid < C) atomicMin(&sh.min_list, w.head[tid].list_bin);
     }
-    sh.bin = (uint32_t)found;
-    sh.above_mass = before;
+    __syncthreads();
+    // prefix counts and masses through each bin, in place of the bins' own
+    if (wave == 0) {
+      const uint32_t c0 = sh.cnt[2 * lane], c1 = sh.cnt[2 * lane + 1];
+      const uint64_t m0 = sh.mass[2 * lane], m1 = sh.mass[2 * lane + 1];
+      const uint64_t cs = wave_scan_u64(c0 + c1), ms = wave_scan_u64(m0 + m1);
+      sh.cnt[2 * lane] = (uint32_t)(cs - c1);
+      sh.cnt[2 * lane + 1] = (uint32_t)cs;
+      sh.mass[2 * lane] = ms - m1;
+      sh.mass[2 * lane + 1] = ms;
+    }
+    __syncthreads();
+    const uint32_t valid = sh.cnt[kBins - 1];
+    const bool by_k = r.q.k < valid;
+    bool by_p = r.q.p < 1.0;
+    // the deepest bin that can hold a kept token
+    auto first_bin = [&](auto before) {  // first bin, of the last at most, that is not `before`
+      int lo = 0, hi = kBins - 1;
+      while (lo < hi) {
+        const int mid = (lo + hi) / 2;
+        if (before(mid)) lo = mid + 1;
+        else hi = mid;
+      }
+      return lo;
+    };
+    auto bin_by_count = [&](uint64_t n) { return first_bin([&](int b) { return sh.cnt[b] < n; }); };
+    auto bin_by_mass = [&](double want) {
+      return first_bin([&](int b) { return sh.cnt[b] == 0 || (double)sh.mass[b] < want; });
+    };
+    // min_p reaches no deeper than this bin (a bin that its border touches included)
+    int deepest = kBins - 1;
+    if (r.q.min_p > 0.0) deepest = r.q.min_p < 1.0 ? bin_of(log2(r.q.min_p) - 1e-9) : 0;
+    if (by_k) {
+      deepest = bin_by_count(r.q.k);
+    } else if (by_p) {
+      const int b = bin_by_mass(r.q.p * (double)sh.mass[kBins - 1]);
+      if (b <= deepest) deepest = b;
+      else by_p = false;  // min_p ends before
+    }
+    N = sh.cnt[deepest];
+    from_list = deepest <= sh.min_list && N <= kCands;
+    auto bin_size = [&](int b) { return sh.cnt[b] - (b ? sh.cnt[b - 1] : 0); };
+    if (from_list) {
+      // candidates: the lists' keys down to that bin
+      for (int c = wave; c < C; c += kDraw / 64) {
+        const Chunk h = w.head[c];
+        for (uint32_t i0 = 0; i0 < h.n_list; i0 += 64) {
+          const uint32_t i = i0 + lane;
+          const uint64_t k = i < h.n_list ? w.list[(size_t)c * kList + i] : 0;
+          const bool in = k && bin_of(exponent_of(key_val(k), r.ref, r.q.c)) <= deepest;
+          const unsigned long long votes = __ballot(in);
+          uint32_t at = 0;
+          if (lane == 0 && votes) at = atomicAdd(&sh.n, (uint32_t)__popcll(votes));
+          at = (uint32_t)__shfl((int)at, 0);
+          if (in) sh.cand[at + __popcll(votes & ((1ull << lane) - 1))] = k;
+        }
+      }
+      __syncthreads();
+    }
+    uint64_t all = sh.mass[kBins - 1];  // mass that top-p is a share of
+    if (by_k) {
+      const int b = bin_by_count(r.q.k);
+      const uint64_t above = b ? sh.cnt[b - 1] : 0, above_mass = b ? sh.mass[b - 1] : 0;
+      if (from_list && bin_size(b) <= kDraw) {
+        r.threshold = search_bin<false>(sh, r, N, b, r.q.k, 0.0, above, above_mass, 0, &all);
+      } else {
+        from_list = false;
+        r.threshold = search_row<false>(sh, r, r.q.k, 0.0, 0);
+        if (by_p) {
+          uint64_t m = 0;
+          for (int i = tid; i < r.V; i += kDraw) {
+            const float z = clean(r.z[i]);
+            if (z != -INFINITY && rank_key(z, i) >= r.threshold) m += mass_of(exponent_of(z, r.ref, r.q.c));
+          }
+          block_scan(sh, m);
+          all = sh.red[kDraw / 64];
+        }
+      }
+    }
+    if (by_p) {
+      const double want = r.q.p * (double)all;
+      const int b = bin_by_mass(want);
+      const uint64_t above = b ? sh.cnt[b - 1] : 0, above_mass = b ? sh.mass[b - 1] : 0;
+      if (from_list && bin_size(b) <= kDraw) {
+        uint64_t unused;
+        r.threshold = search_bin<true>(sh, r, N, b, 0, want, above, above_mass, r.threshold, &unused);
+      } else {
+        from_list = false;
+        r.threshold = search_row<true>(sh, r, 0, want, r.threshold);
+      }
+    }
+    __syncthreads();
+    for (int i = tid; i < n_seg; i += kDraw) sh.seg[i] = 0;
+    __syncthreads();
+    if (from_list) {
+      uint64_t count = 0;
+      for (uint32_t i = tid; i < N; i += kDraw) {
+        const uint64_t k = sh.cand[i];
+        if (k < r.threshold) continue;
+        const float z = key_val(k);
+        const double t = exponent_of(z, r.ref, r.q.c);
+        if (r.q.min_p > 0.0 && z != r.ref && exp2_64(t, 0) < r.q.min_p) continue;
+        ++count;
+        atomicAdd((unsigned long long*)&sh.seg[key_id(k) / kSeg], (unsigned long long)mass_of(t));
+      }
+      block_scan(sh, count);
+      n_kept = (uint32_t)sh.red[kDraw / 64];
+    }
+  } else {
+    // the chunk from the chunks' masses (at most 128 of them)
+    const uint64_t m = tid < C ? w.head[tid].mass : 0;
+    const uint64_t x = block_scan(sh, m);
+    total = sh.red[kDraw / 64];
+    const double want = r.q.u * (double)total;
+    if (m && (double)x > want && !((double)(x - m) > want)) {
+      sh.pick = tid;
+      sh.above_mass = x - m;
+    }
+    __syncthreads();
+    first_seg = (int)sh.pick * (kChunk / kSeg);
+    last_seg = min(n_seg, first_seg + kChunk / kSeg);
+    before = sh.above_mass;
+    block_scan(sh, tid < C ? w.head[tid].tokens : 0);
+    n_kept = (uint32_t)sh.red[kDraw / 64];
+    for (int i = tid; i < n_seg; i += kDraw) sh.seg[i] = 0;
+    __syncthreads();
+  }
+  if (!from_list) {
+    // segment masses from the row, a wave a segment
+    uint64_t count = 0;
+    for (int s = first_seg + wave; s < last_seg; s += kDraw / 64) {
+      uint64_t m = 0;
+#pragma unroll
+      for (int j = 0; j < kSeg / 64; ++j) {
+        const int i = s * kSeg + j * 64 + lane;
+        bool kept = false;
+        if (i < r.V) m += r.weight(i, kept);
+        count += kept;
+      }
+      m = wave_sum_u64(m);
+      if (lane == 0) sh.seg[s] = m;
+    }
+    if (filtered) {
+      block_scan(sh, count);
+      n_kept = (uint32_t)sh.red[kDraw / 64];
+    }
   }
   __syncthreads();
-  if (r.tid == (int)sh.bin) {
-    const double want = p.u * (double)total;
-    uint64_t c = sh.above_mass;
-    int tok = -1;
-    uint32_t d = 0;
-    for (int i = i0; i < i1; ++i) {
-      const uint64_t x = weight(i, d);
-      if (!x) continue;
-      tok = i;
-      c += x;
-      if ((double)c > want) break;
-    }
-    a.tok[row] = tok;
+  // the segment: thread t holds segments 2 t and 2 t + 1
+  {
+    const uint64_t s0 = 2 * tid < n_seg ? sh.seg[2 * tid] : 0;
+    const uint64_t s1 = 2 * tid + 1 < n_seg ? sh.seg[2 * tid + 1] : 0;
+    const uint64_t x = before + block_scan(sh, s0 + s1);
+    if (filtered) total = sh.red[kDraw / 64];
+    const double want = r.q.u * (double)total;
+    const uint64_t b1 = x - s1, b0 = b1 - s0;
+    if (s0 && (double)b1 > want && !((double)b0 > want)) sh.pick = 2 * tid, sh.above_mass = b0;
+    if (s1 && (double)x > want && !((double)b1 > want)) sh.pick = 2 * tid + 1, sh.above_mass = b1;
+  }
+  __syncthreads();
+  const int seg = (int)sh.pick;
+  const uint64_t c0 = sh.above_mass;
+  bool kept = false;
+  const int id = seg * kSeg + tid;
+  const uint64_t m = tid < kSeg && id < r.V ? r.weight(id, kept) : 0;
+  const uint64_t x = c0 + block_scan(sh, m);
+  const double want = r.q.u * (double)total;
+  if (m && (double)x > want && !((double)(x - m) > want)) {
+    a.tok[row] = id;
     if (a.kept) a.kept[row] = (int32_t)n_kept;
     if (a.logp)
-      a.logp[row] = (float)(((double)clean(r.z[tok]) - r.inv_ref) / r.T - log((double)total * 0x1p-43));
+      a.logp[row] = (float)(exponent_of(clean(r.z[id]), r.ref, r.q.c) * 0.6931471805599453 - log((double)total * 0x1p-43));
   }
 }
 
 }  // namespace
 
+size_t sample_row_bytes(int32_t vocab) { return row_bytes(chunks_of(vocab)); }
+
 hipError_t launch_sample(const SampleArgs& a, hipStream_t s) {
-  hipLaunchKernelGGL(sample_kernel, dim3(a.rows), dim3(kThreads), 0, s, a);
+  const int C = chunks_of(a.vocab);
+  hipLaunchKernelGGL(top_kernel, dim3(C, a.rows), dim3(kTally), 0, s, a);
+  hipLaunchKernelGGL(tally_kernel, dim3(C, a.rows), dim3(kTally), 0, s, a);
+  hipLaunchKernelGGL(draw_kernel, dim3(a.rows), dim3(kDraw), 0, s, a, C);
   return hipGetLastError();
 }
 

@@ -221,7 +221,7 @@ msd_status msd_paged_attention(const msd_paged_kv* kv, int32_t layer, const msd_
 
 size_t msd_sample_workspace_bytes(int32_t rows, int32_t vocab) {
   if (rows < 1 || vocab < 1) return 0;
-  return 16;
+  return (size_t)rows * sample_row_bytes(vocab);
 }
 
 msd_status msd_sample(const float* logits, int64_t row_stride, int32_t rows, int32_t vocab,
@@ -248,6 +248,7 @@ msd_status msd_sample(const float* logits, int64_t row_stride, int32_t rows, int
   a.tok = tok;
   a.logp = logp;
   a.kept = kept;
+  a.ws = ws;
   return hip_fail(launch_sample(a, stream));
 }
 
