@@ -8,18 +8,21 @@
 // tokens of mass one fill 2^63).
 //
 //  1 top    a workgroup a chunk of 8192 logits: its largest.
-//  2 tally  the chunk again (held in registers, 16 a thread): masses, and for
-//           filtered rows a histogram of counts and masses over half octaves of 2^t
-//           down to 2^-64, and the keys of the chunk's highest half octaves,
-//           as many as fit 512 keys.
-//  3 draw   a workgroup a row: the histograms added up and scanned from the top give
-//           the half octave in which top-k cuts, then (of what that
-//           leaves) top-p. Where the chunks' lists reach down to it, the cut is
-//           found among them: the keys of that half octave are ranked by counting,
-//           their masses scanned in that order. Else (flat laws, whose kept
-//           sets are a large part of the vocabulary) digit by digit over
-//           the row. The draw: masses of 512-id segments, the segment, the id.
-//           Unfiltered rows take the chunk from the chunks' masses.
+//  2 tally  the chunk again (held in registers, 16 a thread): its mass where the row
+//           needs the mass of all tokens (unfiltered, or top-p without top-k); for
+//           filtered rows a histogram over half octaves of 2^t down to
+//           2^-64, of counts and, for top-p without top-k, masses; and the keys of
+//           the chunk's highest half octaves, in their order, as many as fit 512.
+//  3 draw   a workgroup a row: the histograms added up give the half octave that
+//           top-k (else top-p, min-p) cuts. Where the chunks' lists reach
+//           down to it, its keys and those above come into LDS; a cut is found by a
+//           histogram over 1024 parts of its half octave, the few keys of one
+//           part then ranked by counting. Else (flat laws, whose kept sets are a
+//           large part of the vocabulary) digit by digit over the row. The draw:
+//           masses of 512-id segments, the segment, the id. Unfiltered rows
+//           take the chunk from the chunks' masses.
+// 144 rows of 152K logits: 87.6 MB, read twice (the second time mostly from the
+// memory-side cache).
 #include "sample.h"
 
 namespace msd {
@@ -32,17 +35,18 @@ constexpr int kDraw = 1024;       // threads of the draw
 constexpr int kCands = 8192;      // keys that the draw holds
 constexpr int kSeg = 512;         // ids of a segment
 constexpr int kSegs = (1 << 20) / kSeg;
+constexpr int kMaxChunks = (1 << 20) / kChunk;
 constexpr int kDigit = 2048;      // digit values of the search over a row
 
 struct Chunk {
-  uint32_t n_list;   // keys in its list
-  int32_t list_bin;  // the list holds all its tokens of bins <= list_bin
+  int32_t list_bin;  // the list holds all its tokens of bins <= list_bin, in order of bins
+  int32_t unused;
   uint64_t mass;     // of all its tokens
   uint64_t tokens;   // above -inf
 };
 
-// Workspace of a row: [chunks] top keys, Chunk records, counts [kBins], masses
-// [kBins], lists [kList].
+// Workspace of a row: [chunks] top keys, Chunk records, counts through each bin
+// [kBins], masses of the bins [kBins], lists [kList].
 struct Work {
   uint32_t* top;
   Chunk* head;
@@ -66,7 +70,14 @@ __device__ __forceinline__ Work work_of(const SampleArgs& a, int row, int C) {
   return w;
 }
 
-__device__ __forceinline__ int bin_of(double t) { return (int)fmin(-2.0 * t, (double)(kBins - 1)); }
+// Half octave of a logit, in fp32: any function does that never rises with z and is
+// the same everywhere. x = -2 t (from halves, which do not overflow); its part
+// inside the bin is the fraction.
+__device__ __forceinline__ float depth_of(float z, float ref, float c4) { return (0.5f * ref - 0.5f * z) * c4; }
+__device__ __forceinline__ int bin_of(float x) { return (int)fminf(x, (float)(kBins - 1)); }
+__device__ __forceinline__ float c4_of(const Request& q) { return (float)fmin(4.0 * q.c, 3e38); }
+// whether the row needs the mass of tokens that no list may hold
+__device__ __forceinline__ bool mass_by_bin(const Request& q, int V) { return q.p < 1.0 && q.k >= (uint32_t)V; }
 
 __device__ __forceinline__ uint32_t wave_max_u32(uint32_t v) {
 #pragma unroll
@@ -110,9 +121,10 @@ __global__ __launch_bounds__(kTally) void top_kernel(SampleArgs a) {
 __global__ __launch_bounds__(kTally) void tally_kernel(SampleArgs a) {
   __shared__ uint32_t cnt[kBins];
   __shared__ unsigned long long mass[kBins];
+  __shared__ uint32_t cursor[kBins];
   __shared__ uint64_t red[kTally / 64];
   __shared__ uint32_t red_n[kTally / 64];
-  __shared__ uint32_t n_list;
+  __shared__ uint32_t last_bin;
   __shared__ int list_bin;
   const int C = gridDim.x, c = blockIdx.x, row = blockIdx.y, tid = threadIdx.x;
   const Work w = work_of(a, row, C);
@@ -129,9 +141,10 @@ __global__ __launch_bounds__(kTally) void tally_kernel(SampleArgs a) {
   if (top <= kDead) return;  // no token
   const float ref = from_ordered_bits(top);
   const Request q = request_of(a, row);
-  const bool filtered = q.filtered();
+  const float c4 = c4_of(q);
+  const bool filtered = q.filtered(), by_bin = mass_by_bin(q, a.vocab);
   if (tid < kBins) cnt[tid] = 0, mass[tid] = 0;
-  if (tid == 0) n_list = 0;
+  if (tid == 0) last_bin = 0;
   __syncthreads();
   uint64_t sum = 0;
   uint32_t tokens = 0;
@@ -139,32 +152,31 @@ __global__ __launch_bounds__(kTally) void tally_kernel(SampleArgs a) {
 #pragma unroll
   for (int j = 0; j < kEach; ++j) {
     if (v[j] == -INFINITY) continue;
-    const double t = exponent_of(v[j], ref, q.c);
-    const uint64_t m = mass_of(t);
-    sum += m;
     ++tokens;
+    uint64_t m = 0;
+    if (!filtered || by_bin) sum += m = mass_of(exponent_of(v[j], ref, q.c));
     if (!filtered) continue;
-    const int b = bin_of(t);
-    if (b == kBins - 1) {
-      ++low;
-      continue;
-    }
-    atomicAdd(&cnt[b], 1u);
+    const int b = bin_of(depth_of(v[j], ref, c4));
+    if (b == kBins - 1) ++low;
+    else atomicAdd(&cnt[b], 1u);
     if (m) atomicAdd(&mass[b], (unsigned long long)m);
   }
   sum = wave_sum_u64(sum);
   tokens = (uint32_t)wave_sum_u64(tokens);
-  if (low) atomicAdd(&cnt[kBins - 1], low);
+  if (low) atomicAdd(&last_bin, low);
   if ((tid & 63) == 0) red[tid >> 6] = sum, red_n[tid >> 6] = tokens;
   __syncthreads();
   if (tid < 64) {
-    // the deepest bin down to which the chunk's tokens fit its list
-    const uint32_t c0 = cnt[2 * tid], c1 = cnt[2 * tid + 1];
-    const uint64_t x = wave_scan_u64(c0 + c1);
-    const int fit = (x - c1 <= kList) + (x <= kList);  // prefix counts: of this lane's two bins
-    int f = fit;
+    // counts through each bin; the deepest bin down to which they fit the list
+    const uint32_t c0 = cnt[2 * tid], c1 = tid == 63 ? last_bin : cnt[2 * tid + 1];
+    const uint32_t x = (uint32_t)wave_scan_u64(c0 + c1);
+    int f = (x - c1 <= kList) + (x <= kList);
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) f += __shfl_xor(f, o);
+    cursor[2 * tid] = x - c1 - c0;
+    cursor[2 * tid + 1] = x - c1;
+    cnt[2 * tid] = x - c1;
+    cnt[2 * tid + 1] = x;
     if (tid == 0) {
       list_bin = f - 1;
       for (int i = 1; i < kTally / 64; ++i) red[0] += red[i], red_n[0] += red_n[i];
@@ -175,27 +187,27 @@ __global__ __launch_bounds__(kTally) void tally_kernel(SampleArgs a) {
     const int lb = list_bin;
 #pragma unroll
     for (int j = 0; j < kEach; ++j) {
-      if (v[j] == -INFINITY || bin_of(exponent_of(v[j], ref, q.c)) > lb) continue;
-      w.list[(size_t)c * kList + atomicAdd(&n_list, 1u)] = rank_key(v[j], c * kChunk + j * kTally + tid);
+      const int b = v[j] == -INFINITY ? kBins : bin_of(depth_of(v[j], ref, c4));
+      if (b <= lb) w.list[(size_t)c * kList + atomicAdd(&cursor[b], 1u)] = rank_key(v[j], c * kChunk + j * kTally + tid);
     }
     if (tid < kBins) {
       w.cnt[(size_t)c * kBins + tid] = cnt[tid];
-      w.mass[(size_t)c * kBins + tid] = mass[tid];
+      if (by_bin) w.mass[(size_t)c * kBins + tid] = mass[tid];
     }
-    __syncthreads();
   }
-  if (tid == 0) w.head[c] = Chunk{n_list, list_bin, red[0], red_n[0]};
+  if (tid == 0) w.head[c] = Chunk{list_bin, 0, red[0], red_n[0]};
 }
 
 struct Shared {
   uint64_t cand[kCands];       // keys; in the search over a row: digit masses
-  uint64_t seg[kSegs];         // segment masses; before: masses by rank
+  uint64_t seg[kSegs];         // segment masses; before, the search among the keys
   uint64_t red[kDraw / 64 + 1];
   uint64_t mass[kBins];        // tokens of the bins above, then of the bin
   uint32_t cnt[kBins];
-  uint64_t above_mass, key, want_bits;
-  uint32_t above, n, m, pick;
+  uint64_t above_mass, above, key;
+  uint32_t n, m, pick;
   int min_list;
+  uint32_t from[kMaxChunks + 1];  // candidates of the chunks before
 };
 static_assert(kCands * 8 >= kDigit * 12, "digit histograms fit the key list");
 
@@ -221,8 +233,11 @@ struct Row {
   int V;
   float ref;   // the largest logit
   uint32_t top;
+  float c4;
   Request q;
   uint64_t threshold;  // smallest kept key
+  __device__ uint64_t mass(uint64_t key) const { return mass_of(exponent_of(key_val(key), ref, q.c)); }
+  __device__ float depth(uint64_t key) const { return depth_of(key_val(key), ref, c4); }
   __device__ uint64_t weight(int i, bool& kept) const {
     const float x = clean(z[i]);
     kept = false;
@@ -320,22 +335,56 @@ __device__ uint64_t search_row(Shared& sh, const Row& r, uint64_t n, double want
   return sh.key;
 }
 
-// The same among the candidate keys: those of bin `bin`, at most kDraw, ranked by
-// counting; `above` tokens and `above_mass` lie in the bins before.
+// The same among the candidate keys >= floor of bin `bin`; `above` tokens and
+// `above_mass` lie in the bins before. First the part of the bin (1024, a thread
+// each) in which the prefix ends, then the keys of that part in order. False:
+// more keys in one part than threads (equal logits).
 template <bool BY_MASS>
-__device__ uint64_t search_bin(Shared& sh, const Row& r, uint32_t N, int bin, uint64_t n, double want, uint64_t above,
-                               uint64_t above_mass, uint64_t floor, uint64_t* kept_mass) {
+__device__ bool search_bin(Shared& sh, const Row& r, uint32_t N, int bin, uint64_t n, double want, uint64_t above,
+                           uint64_t above_mass, uint64_t floor, uint64_t* key_out, uint64_t* kept_mass) {
   const int tid = threadIdx.x;
-  uint64_t* mine = sh.seg;  // keys of the bin
+  uint64_t* mass = sh.seg;                                       // [kDraw]
+  uint32_t* cnt = reinterpret_cast<uint32_t*>(sh.seg + kDraw);   // [kDraw]
+  auto part_of = [&](uint64_t k) {  // -1: not of the bin
+    const float x = r.depth(k);
+    return bin_of(x) != bin ? -1 : (int)fminf((x - (float)bin) * kDraw, (float)(kDraw - 1));
+  };
+  auto inside = [&](uint64_t cb, uint64_t mb) { return BY_MASS ? (cb == 0 || (double)mb < want) : cb < n; };
   __syncthreads();
-  if (tid == 0) sh.m = 0;
+  mass[tid] = 0;
+  cnt[tid] = 0;
+  if (tid == 0) sh.m = 0, sh.n = 0;
   __syncthreads();
   for (uint32_t i = tid; i < N; i += kDraw) {
     const uint64_t k = sh.cand[i];
-    if (k >= floor && bin_of(exponent_of(key_val(k), r.ref, r.q.c)) == bin) mine[atomicAdd(&sh.m, 1u)] = k;
+    if (k < floor) continue;
+    const int p = part_of(k);
+    if (p < 0) continue;
+    atomicAdd(&cnt[p], 1u);
+    atomicAdd((unsigned long long*)&mass[p], (unsigned long long)r.mass(k));
   }
   __syncthreads();
-  const uint32_t m = sh.m;
+  {
+    const uint64_t c0 = cnt[tid], m0 = mass[tid];
+    const uint64_t cb = above + block_scan(sh, c0) - c0;
+    const uint64_t mb = above_mass + block_scan(sh, m0) - m0;
+    const bool in = c0 && inside(cb, mb);  // a prefix of the parts
+    if (in) atomicMax(&sh.m, (uint32_t)tid);
+    __syncthreads();
+    if (in && sh.m == (uint32_t)tid) sh.above = cb, sh.above_mass = mb, sh.pick = (uint32_t)c0;
+    __syncthreads();
+  }
+  const int part = (int)sh.m;
+  const uint32_t m = sh.pick;
+  above = sh.above;
+  above_mass = sh.above_mass;
+  if (m > kDraw) return false;
+  uint64_t* mine = sh.seg;
+  for (uint32_t i = tid; i < N; i += kDraw) {
+    const uint64_t k = sh.cand[i];
+    if (k >= floor && part_of(k) == part) mine[atomicAdd(&sh.n, 1u)] = k;
+  }
+  __syncthreads();
   const uint64_t key = tid < (int)m ? mine[tid] : 0;
   uint32_t rank = 0;
   for (uint32_t i = 0; i < m; ++i) rank += mine[i] > key;
@@ -343,23 +392,22 @@ __device__ uint64_t search_bin(Shared& sh, const Row& r, uint32_t N, int bin, ui
   uint64_t* by_rank = sh.seg;               // masses
   uint64_t* key_by_rank = sh.seg + kDraw;
   if (tid < (int)m) {
-    by_rank[rank] = mass_of(exponent_of(key_val(key), r.ref, r.q.c));
+    by_rank[rank] = r.mass(key);
     key_by_rank[rank] = key;
   }
   __syncthreads();
   const uint64_t w = tid < (int)m ? by_rank[tid] : 0;
   const uint64_t x = above_mass + block_scan(sh, w);  // mass through rank tid
-  bool in;
-  if (BY_MASS) in = tid < (int)m && ((double)(x - w) < want || above + tid == 0);
-  else in = tid < (int)m && above + tid < n;
-  // ranks inside are a prefix: the last of them
-  if (in && (tid + 1 == (int)m || !(BY_MASS ? (double)x < want : above + tid + 1 < n))) {
+  // the ranks inside are a prefix: the last of them
+  if (tid < (int)m && inside(above + tid, x - w) && (tid + 1 == (int)m || !inside(above + tid + 1, x))) {
     sh.key = key_by_rank[tid];
     sh.above_mass = x;
   }
   __syncthreads();
+  *key_out = sh.key;
   *kept_mass = sh.above_mass;
-  return sh.key;
+  __syncthreads();
+  return true;
 }
 static_assert(kSegs >= 2 * kDraw, "ranks and their keys fit the segment masses");
 
@@ -383,6 +431,7 @@ __global__ __launch_bounds__(kDraw) void draw_kernel(SampleArgs a, int C) {
     return;
   }
   r.ref = from_ordered_bits(r.top);
+  r.c4 = c4_of(r.q);
   r.threshold = 0;
   const bool filtered = r.q.filtered();
   uint32_t n_kept = 0;
@@ -393,8 +442,9 @@ __global__ __launch_bounds__(kDraw) void draw_kernel(SampleArgs a, int C) {
   uint32_t N = 0;
 
   if (filtered) {
+    const bool by_bin = mass_by_bin(r.q, r.V);
     if (tid < kBins) sh.cnt[tid] = 0, sh.mass[tid] = 0;
-    if (tid == 0) sh.min_list = kBins, sh.n = 0;
+    if (tid == 0) sh.min_list = kBins;
     __syncthreads();
     {
       uint32_t n = 0;
@@ -402,28 +452,26 @@ __global__ __launch_bounds__(kDraw) void draw_kernel(SampleArgs a, int C) {
       const int b = tid % kBins;
       for (int c = tid / kBins; c < C; c += kDraw / kBins) {
         n += w.cnt[(size_t)c * kBins + b];
-        m += w.mass[(size_t)c * kBins + b];
+        if (by_bin) m += w.mass[(size_t)c * kBins + b];
       }
       if (n) atomicAdd(&sh.cnt[b], n);
       if (m) atomicAdd((unsigned long long*)&sh.mass[b], (unsigned long long)m);
       if (tid < C) atomicMin(&sh.min_list, w.head[tid].list_bin);
     }
     __syncthreads();
-    // prefix counts and masses through each bin, in place of the bins' own
-    if (wave == 0) {
-      const uint32_t c0 = sh.cnt[2 * lane], c1 = sh.cnt[2 * lane + 1];
-      const uint64_t m0 = sh.mass[2 * lane], m1 = sh.mass[2 * lane + 1];
-      const uint64_t cs = wave_scan_u64(c0 + c1), ms = wave_scan_u64(m0 + m1);
-      sh.cnt[2 * lane] = (uint32_t)(cs - c1);
-      sh.cnt[2 * lane + 1] = (uint32_t)cs;
-      sh.mass[2 * lane] = ms - m1;
-      sh.mass[2 * lane + 1] = ms;
-    }
-    __syncthreads();
+    auto mass_prefix = [&]() {  // bins' masses to those through each bin
+      if (wave == 0) {
+        const uint64_t m0 = sh.mass[2 * lane], m1 = sh.mass[2 * lane + 1];
+        const uint64_t x = wave_scan_u64(m0 + m1);
+        sh.mass[2 * lane] = x - m1;
+        sh.mass[2 * lane + 1] = x;
+      }
+      __syncthreads();
+    };
+    if (by_bin) mass_prefix();
     const uint32_t valid = sh.cnt[kBins - 1];
     const bool by_k = r.q.k < valid;
     bool by_p = r.q.p < 1.0;
-    // the deepest bin that can hold a kept token
     auto first_bin = [&](auto before) {  // first bin, of the last at most, that is not `before`
       int lo = 0, hi = kBins - 1;
       while (lo < hi) {
@@ -433,71 +481,76 @@ __global__ __launch_bounds__(kDraw) void draw_kernel(SampleArgs a, int C) {
       }
       return lo;
     };
-    auto bin_by_count = [&](uint64_t n) { return first_bin([&](int b) { return sh.cnt[b] < n; }); };
     auto bin_by_mass = [&](double want) {
       return first_bin([&](int b) { return sh.cnt[b] == 0 || (double)sh.mass[b] < want; });
     };
-    // min_p reaches no deeper than this bin (a bin that its border touches included)
+    // the deepest bin that can hold a kept token; min_p's is one more than its
+    // border's, whatever way that rounds
     int deepest = kBins - 1;
-    if (r.q.min_p > 0.0) deepest = r.q.min_p < 1.0 ? bin_of(log2(r.q.min_p) - 1e-9) : 0;
+    if (r.q.min_p > 0.0) deepest = r.q.min_p < 1.0 ? min(kBins - 1, bin_of((float)(-2.0 * log2(r.q.min_p))) + 1) : 0;
+    int k_bin = 0;
     if (by_k) {
-      deepest = bin_by_count(r.q.k);
-    } else if (by_p) {
+      k_bin = first_bin([&](int b) { return sh.cnt[b] < r.q.k; });
+      deepest = k_bin;
+    } else if (by_p && by_bin) {
       const int b = bin_by_mass(r.q.p * (double)sh.mass[kBins - 1]);
       if (b <= deepest) deepest = b;
       else by_p = false;  // min_p ends before
+    } else if (by_p) {
+      deepest = kBins - 1;  // top-k that keeps all of a row with few tokens: their masses come from the keys
     }
     N = sh.cnt[deepest];
     from_list = deepest <= sh.min_list && N <= kCands;
-    auto bin_size = [&](int b) { return sh.cnt[b] - (b ? sh.cnt[b - 1] : 0); };
     if (from_list) {
-      // candidates: the lists' keys down to that bin
+      // candidates: the first keys of every chunk's list
+      uint32_t n = 0;
+      if (tid < C) n = w.cnt[(size_t)tid * kBins + deepest];
+      const uint64_t x = block_scan(sh, n);
+      if (tid < C) sh.from[tid] = (uint32_t)(x - n);
+      if (tid == C) sh.from[C] = (uint32_t)x;
+      __syncthreads();
       for (int c = wave; c < C; c += kDraw / 64) {
-        const Chunk h = w.head[c];
-        for (uint32_t i0 = 0; i0 < h.n_list; i0 += 64) {
-          const uint32_t i = i0 + lane;
-          const uint64_t k = i < h.n_list ? w.list[(size_t)c * kList + i] : 0;
-          const bool in = k && bin_of(exponent_of(key_val(k), r.ref, r.q.c)) <= deepest;
-          const unsigned long long votes = __ballot(in);
-          uint32_t at = 0;
-          if (lane == 0 && votes) at = atomicAdd(&sh.n, (uint32_t)__popcll(votes));
-          at = (uint32_t)__shfl((int)at, 0);
-          if (in) sh.cand[at + __popcll(votes & ((1ull << lane) - 1))] = k;
-        }
+        const uint32_t at = sh.from[c], m = sh.from[c + 1] - at;
+        for (uint32_t i = lane; i < m; i += 64) sh.cand[at + i] = w.list[(size_t)c * kList + i];
       }
       __syncthreads();
     }
-    uint64_t all = sh.mass[kBins - 1];  // mass that top-p is a share of
-    if (by_k) {
-      const int b = bin_by_count(r.q.k);
-      const uint64_t above = b ? sh.cnt[b - 1] : 0, above_mass = b ? sh.mass[b - 1] : 0;
-      if (from_list && bin_size(b) <= kDraw) {
-        r.threshold = search_bin<false>(sh, r, N, b, r.q.k, 0.0, above, above_mass, 0, &all);
-      } else {
-        from_list = false;
-        r.threshold = search_row<false>(sh, r, r.q.k, 0.0, 0);
-        if (by_p) {
-          uint64_t m = 0;
-          for (int i = tid; i < r.V; i += kDraw) {
-            const float z = clean(r.z[i]);
-            if (z != -INFINITY && rank_key(z, i) >= r.threshold) m += mass_of(exponent_of(z, r.ref, r.q.c));
-          }
-          block_scan(sh, m);
-          all = sh.red[kDraw / 64];
-        }
+    uint64_t all = by_bin ? sh.mass[kBins - 1] : 0;  // mass that top-p is a share of
+    if (by_p && !by_bin && from_list) {
+      // the bins' masses from the keys
+      for (uint32_t i = tid; i < N; i += kDraw) {
+        const uint64_t k = sh.cand[i];
+        atomicAdd((unsigned long long*)&sh.mass[bin_of(r.depth(k))], (unsigned long long)r.mass(k));
       }
+      __syncthreads();
+      mass_prefix();
+      all = sh.mass[kBins - 1];
+    }
+    if (by_k) {
+      const uint64_t above = k_bin ? sh.cnt[k_bin - 1] : 0, above_mass = k_bin ? sh.mass[k_bin - 1] : 0;
+      if (from_list)
+        from_list = search_bin<false>(sh, r, N, k_bin, r.q.k, 0.0, above, above_mass, 0, &r.threshold, &all);
+      if (!from_list) r.threshold = search_row<false>(sh, r, r.q.k, 0.0, 0);
+    }
+    if (by_p && !by_bin && !from_list) {
+      uint64_t m = 0;
+      for (int i = tid; i < r.V; i += kDraw) {
+        const float z = clean(r.z[i]);
+        if (z != -INFINITY && rank_key(z, i) >= r.threshold) m += mass_of(exponent_of(z, r.ref, r.q.c));
+      }
+      block_scan(sh, m);
+      all = sh.red[kDraw / 64];
+      __syncthreads();
     }
     if (by_p) {
       const double want = r.q.p * (double)all;
-      const int b = bin_by_mass(want);
-      const uint64_t above = b ? sh.cnt[b - 1] : 0, above_mass = b ? sh.mass[b - 1] : 0;
-      if (from_list && bin_size(b) <= kDraw) {
+      if (from_list) {
+        const int b = bin_by_mass(want);
+        const uint64_t above = b ? sh.cnt[b - 1] : 0, above_mass = b ? sh.mass[b - 1] : 0;
         uint64_t unused;
-        r.threshold = search_bin<true>(sh, r, N, b, 0, want, above, above_mass, r.threshold, &unused);
-      } else {
-        from_list = false;
-        r.threshold = search_row<true>(sh, r, 0, want, r.threshold);
+        from_list = search_bin<true>(sh, r, N, b, 0, want, above, above_mass, r.threshold, &r.threshold, &unused);
       }
+      if (!from_list) r.threshold = search_row<true>(sh, r, 0, want, r.threshold);
     }
     __syncthreads();
     for (int i = tid; i < n_seg; i += kDraw) sh.seg[i] = 0;
