@@ -554,7 +554,8 @@ size_t msd_sample_workspace_bytes(int32_t rows, int32_t vocab);
 /* logits device fp32, row r at logits + r * row_stride (row_stride >= vocab);
  * u device fp32 [rows]; tok device int32 [rows]; logp (fp32) and kept (int32)
  * device [rows] or NULL; params NULL: all defaults. rows in [1, 65535],
- * vocab in [1, 1048576]. */
+ * vocab in [1, 1048576]; ws of msd_sample_workspace_bytes (it never falls when
+ * an argument grows), 16-byte aligned. */
 msd_status msd_sample(const float* logits, int64_t row_stride, int32_t rows, int32_t vocab,
                       const msd_sample_params* params, const float* u, int32_t* tok, float* logp,
                       int32_t* kept, void* ws, size_t ws_bytes, hipStream_t stream);

@@ -353,9 +353,9 @@ struct SampleArgs {
   int32_t* tok;
   float* logp;               // or null
   int32_t* kept;             // or null
-  void* ws;                  // rows * sample_row_bytes(vocab)
+  void* ws;                  // sample_ws_bytes(rows, vocab)
 };
-size_t sample_row_bytes(int32_t vocab);
+size_t sample_ws_bytes(int32_t rows, int32_t vocab);
 hipError_t launch_sample(const SampleArgs& a, hipStream_t s);
 
 }  // namespace msd

@@ -23,19 +23,24 @@
 //           take the chunk from the chunks' masses.
 // 144 rows of 152K logits: 87.6 MB, read twice (the second time mostly from the
 // memory-side cache).
+#include <algorithm>
+
 #include "sample.h"
 
 namespace msd {
 namespace {
 
-constexpr int kChunk = 8192, kTally = 512, kEach = kChunk / kTally;
+constexpr int kTally = 512;       // threads of a chunk
+// Logits a thread of a chunk holds: 16 (chunks of 8192), or 4 where all chunks of
+// that size are fewer than the compute units (one row of 152K: 19 of 8192 or 75 of 2048).
+constexpr int kFew = 4, kMany = 16;
 constexpr int kBins = 128;        // half octaves; the last takes all below 2^-63.5
 constexpr int kList = 512;        // keys of a chunk's list
 constexpr int kDraw = 1024;       // threads of the draw
 constexpr int kCands = 8192;      // keys that the draw holds
 constexpr int kSeg = 512;         // ids of a segment
 constexpr int kSegs = (1 << 20) / kSeg;
-constexpr int kMaxChunks = (1 << 20) / kChunk;
+constexpr int kMaxChunks = 256;
 constexpr int kDigit = 2048;      // digit values of the search over a row
 
 struct Chunk {
@@ -54,7 +59,12 @@ struct Work {
   uint64_t* mass;
   uint64_t* list;
 };
-__host__ __device__ inline int chunks_of(int vocab) { return (vocab + kChunk - 1) / kChunk; }
+// the larger chunks also where the smaller ones would be more than kMaxChunks
+inline int each_of(int rows, int vocab) {
+  const int many = (vocab + kTally * kMany - 1) / (kTally * kMany), few = (vocab + kTally * kFew - 1) / (kTally * kFew);
+  return (int64_t)rows * many < 256 && few <= kMaxChunks ? kFew : kMany;
+}
+inline int chunks_of(int each, int vocab) { return (vocab + kTally * each - 1) / (kTally * each); }
 __host__ __device__ inline size_t row_bytes(int C) {
   const size_t b = (size_t)C * (kList * 8 + kBins * 12 + sizeof(Chunk) + 4);
   return (b + 15) / 16 * 16;
@@ -84,43 +94,70 @@ __device__ __forceinline__ uint32_t wave_max_u32(uint32_t v) {
   for (int o = 32; o > 0; o >>= 1) v = max(v, (uint32_t)__shfl_xor((int)v, o));
   return v;
 }
-__device__ __forceinline__ uint64_t wave_sum_u64(uint64_t v) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o);
-  return v;
+// Inclusive scan of a wave by lane moves inside the vector unit: rows of 16 shifted
+// by 1, 2, 4 and 8, then the last lane of a row added to the next row, and that
+// of the lower half to the upper.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ uint64_t add_moved(uint64_t v) {
+  const uint32_t lo = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)v, CTRL, ROWS, 0xf, false);
+  const uint32_t hi = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)(v >> 32), CTRL, ROWS, 0xf, false);
+  return v + (((uint64_t)hi << 32) | lo);
 }
-__device__ __forceinline__ uint64_t wave_scan_u64(uint64_t v) {  // inclusive
-  const int lane = threadIdx.x & 63;
+__device__ __forceinline__ uint64_t wave_scan_u64(uint64_t v) {
+  v = add_moved<0x111, 0xf>(v);  // row_shr 1, 2, 4, 8
+  v = add_moved<0x112, 0xf>(v);
+  v = add_moved<0x114, 0xf>(v);
+  v = add_moved<0x118, 0xf>(v);
+  v = add_moved<0x142, 0xa>(v);  // row_bcast 15 into rows 1 and 3
+  return add_moved<0x143, 0xc>(v);  // row_bcast 31 into rows 2 and 3
+}
+__device__ __forceinline__ uint64_t lane_u64(uint64_t v, int lane) {
+  const uint32_t lo = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)v, lane);
+  const uint32_t hi = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(v >> 32), lane);
+  return ((uint64_t)hi << 32) | lo;
+}
+__device__ __forceinline__ uint64_t wave_sum_u64(uint64_t v) { return lane_u64(wave_scan_u64(v), 63); }
+
+// Four consecutive logits, cleaned, those past the row as -inf. Rows start at any
+// fp32 (a 16-byte load takes any 4-byte address).
+typedef float float4_any __attribute__((ext_vector_type(4), aligned(4)));
+__device__ __forceinline__ void load4(const float* z, int i, int V, float* v) {
+  if (i + 4 <= V) {
+    const float4_any x = *reinterpret_cast<const float4_any*>(z + i);
 #pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const uint64_t y = __shfl_up(v, o);
-    if (lane >= o) v += y;
+    for (int e = 0; e < 4; ++e) v[e] = clean(x[e]);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = i + e < V ? clean(z[i + e]) : -INFINITY;
   }
-  return v;
 }
 
+template <int EACH>
 __global__ __launch_bounds__(kTally) void top_kernel(SampleArgs a) {
   __shared__ uint32_t red[kTally / 64];
   const int c = blockIdx.x, row = blockIdx.y, tid = threadIdx.x;
   const float* z = a.logits + (int64_t)row * a.row_stride;
-  uint32_t top = 0;
+  float v[EACH];
 #pragma unroll
-  for (int j = 0; j < kEach; ++j) {
-    const int i = c * kChunk + j * kTally + tid;
-    if (i < a.vocab) top = max(top, ordered_bits(clean(z[i])));
-  }
-  top = wave_max_u32(top);
-  if ((tid & 63) == 0) red[tid >> 6] = top;
+  for (int j = 0; j < EACH; j += 4) load4(z, c * (kTally * EACH) + j * kTally + 4 * tid, a.vocab, v + j);
+  float top = v[0];
+#pragma unroll
+  for (int j = 1; j < EACH; ++j) top = fmaxf(top, v[j]);
+  const uint32_t m = wave_max_u32(ordered_bits(top));
+  if ((tid & 63) == 0) red[tid >> 6] = m;
   __syncthreads();
   if (tid == 0) {
-    for (int w = 1; w < kTally / 64; ++w) top = max(top, red[w]);
-    work_of(a, row, gridDim.x).top[c] = top;
+    uint32_t t = red[0];
+    for (int w = 1; w < kTally / 64; ++w) t = max(t, red[w]);
+    work_of(a, row, gridDim.x).top[c] = t;
   }
 }
 
+constexpr int kCopies = 4;  // of the histogram, by lane: tokens of one bin meet less often
+template <int EACH>
 __global__ __launch_bounds__(kTally) void tally_kernel(SampleArgs a) {
-  __shared__ uint32_t cnt[kBins];
-  __shared__ unsigned long long mass[kBins];
+  __shared__ uint32_t cnt[kBins * kCopies];
+  __shared__ unsigned long long mass[kBins * kCopies];
   __shared__ uint32_t cursor[kBins];
   __shared__ uint64_t red[kTally / 64];
   __shared__ uint32_t red_n[kTally / 64];
@@ -129,28 +166,27 @@ __global__ __launch_bounds__(kTally) void tally_kernel(SampleArgs a) {
   const int C = gridDim.x, c = blockIdx.x, row = blockIdx.y, tid = threadIdx.x;
   const Work w = work_of(a, row, C);
   const float* z = a.logits + (int64_t)row * a.row_stride;
-  float v[kEach];
+  const int first = c * (kTally * EACH) + 4 * tid;  // v[j]: id first + kTally * (j & ~3) + (j & 3)
+  float v[EACH];
 #pragma unroll
-  for (int j = 0; j < kEach; ++j) {
-    const int i = c * kChunk + j * kTally + tid;
-    v[j] = i < a.vocab ? clean(z[i]) : -INFINITY;
-  }
+  for (int j = 0; j < EACH; j += 4) load4(z, first + j * kTally, a.vocab, v + j);
   uint32_t top = 0;
   for (int i = tid & 63; i < C; i += 64) top = max(top, w.top[i]);
+  const Request q = request_of(a, row);
   top = wave_max_u32(top);
   if (top <= kDead) return;  // no token
   const float ref = from_ordered_bits(top);
-  const Request q = request_of(a, row);
   const float c4 = c4_of(q);
   const bool filtered = q.filtered(), by_bin = mass_by_bin(q, a.vocab);
-  if (tid < kBins) cnt[tid] = 0, mass[tid] = 0;
+  for (int i = tid; i < kBins * kCopies; i += kTally) cnt[i] = 0, mass[i] = 0;
   if (tid == 0) last_bin = 0;
   __syncthreads();
   uint64_t sum = 0;
   uint32_t tokens = 0;
   uint32_t low = 0;  // tokens of the last bin, which most tokens of cold laws share
+  const int copy = tid % kCopies;
 #pragma unroll
-  for (int j = 0; j < kEach; ++j) {
+  for (int j = 0; j < EACH; ++j) {
     if (v[j] == -INFINITY) continue;
     ++tokens;
     uint64_t m = 0;
@@ -158,8 +194,8 @@ __global__ __launch_bounds__(kTally) void tally_kernel(SampleArgs a) {
     if (!filtered) continue;
     const int b = bin_of(depth_of(v[j], ref, c4));
     if (b == kBins - 1) ++low;
-    else atomicAdd(&cnt[b], 1u);
-    if (m) atomicAdd(&mass[b], (unsigned long long)m);
+    else atomicAdd(&cnt[b * kCopies + copy], 1u);
+    if (m) atomicAdd(&mass[b * kCopies + copy], (unsigned long long)m);
   }
   sum = wave_sum_u64(sum);
   tokens = (uint32_t)wave_sum_u64(tokens);
@@ -168,40 +204,46 @@ __global__ __launch_bounds__(kTally) void tally_kernel(SampleArgs a) {
   __syncthreads();
   if (tid < 64) {
     // counts through each bin; the deepest bin down to which they fit the list
-    const uint32_t c0 = cnt[2 * tid], c1 = tid == 63 ? last_bin : cnt[2 * tid + 1];
-    const uint32_t x = (uint32_t)wave_scan_u64(c0 + c1);
-    int f = (x - c1 <= kList) + (x <= kList);
+    uint32_t c0 = 0, c1 = 0;
 #pragma unroll
-    for (int o = 32; o > 0; o >>= 1) f += __shfl_xor(f, o);
+    for (int k = 0; k < kCopies; ++k) c0 += cnt[2 * tid * kCopies + k], c1 += cnt[(2 * tid + 1) * kCopies + k];
+    if (tid == 63) c1 = last_bin;
+    const uint32_t x = (uint32_t)wave_scan_u64(c0 + c1);
+    const int f = (int)__popcll(__ballot(x - c1 <= kList)) + (int)__popcll(__ballot(x <= kList));
     cursor[2 * tid] = x - c1 - c0;
     cursor[2 * tid + 1] = x - c1;
-    cnt[2 * tid] = x - c1;
-    cnt[2 * tid + 1] = x;
+    if (filtered) {
+      w.cnt[(size_t)c * kBins + 2 * tid] = x - c1;
+      w.cnt[(size_t)c * kBins + 2 * tid + 1] = x;
+    }
     if (tid == 0) {
       list_bin = f - 1;
-      for (int i = 1; i < kTally / 64; ++i) red[0] += red[i], red_n[0] += red_n[i];
+      uint64_t s = red[0], n = red_n[0];
+      for (int i = 1; i < kTally / 64; ++i) s += red[i], n += red_n[i];
+      w.head[c] = Chunk{f - 1, 0, s, n};
     }
+  }
+  if (!filtered) return;
+  if (by_bin && tid >= 64 && tid < 64 + kBins) {
+    uint64_t m = 0;
+#pragma unroll
+    for (int k = 0; k < kCopies; ++k) m += mass[(tid - 64) * kCopies + k];
+    w.mass[(size_t)c * kBins + tid - 64] = m;
   }
   __syncthreads();
-  if (filtered) {
-    const int lb = list_bin;
+  const int lb = list_bin;
 #pragma unroll
-    for (int j = 0; j < kEach; ++j) {
-      const int b = v[j] == -INFINITY ? kBins : bin_of(depth_of(v[j], ref, c4));
-      if (b <= lb) w.list[(size_t)c * kList + atomicAdd(&cursor[b], 1u)] = rank_key(v[j], c * kChunk + j * kTally + tid);
-    }
-    if (tid < kBins) {
-      w.cnt[(size_t)c * kBins + tid] = cnt[tid];
-      if (by_bin) w.mass[(size_t)c * kBins + tid] = mass[tid];
-    }
+  for (int j = 0; j < EACH; ++j) {
+    const int b = v[j] == -INFINITY ? kBins : bin_of(depth_of(v[j], ref, c4));
+    if (b <= lb)
+      w.list[(size_t)c * kList + atomicAdd(&cursor[b], 1u)] = rank_key(v[j], first + kTally * (j & ~3) + (j & 3));
   }
-  if (tid == 0) w.head[c] = Chunk{list_bin, 0, red[0], red_n[0]};
 }
 
 struct Shared {
   uint64_t cand[kCands];       // keys; in the search over a row: digit masses
   uint64_t seg[kSegs];         // segment masses; before, the search among the keys
-  uint64_t red[kDraw / 64 + 1];
+  uint64_t red[2][kDraw / 64];
   uint64_t mass[kBins];        // tokens of the bins above, then of the bin
   uint32_t cnt[kBins];
   uint64_t above_mass, above, key;
@@ -211,22 +253,23 @@ struct Shared {
 };
 static_assert(kCands * 8 >= kDigit * 12, "digit histograms fit the key list");
 
-// inclusive block scan over kDraw threads; total in sh.red[kDraw / 64]
-__device__ __forceinline__ uint64_t block_scan(Shared& sh, uint64_t v) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const uint64_t x = wave_scan_u64(v);
-  __syncthreads();
-  if (lane == 63) sh.red[wave] = x;
-  __syncthreads();
-  if (wave == 0) {
-    const uint64_t y = lane < kDraw / 64 ? sh.red[lane] : 0;
-    const uint64_t s = wave_scan_u64(y);
-    if (lane < kDraw / 64) sh.red[lane] = s - y;
-    if (lane == kDraw / 64 - 1) sh.red[kDraw / 64] = s;
+// Inclusive scan over the block, and the block's sum. One barrier: wave sums go to
+// one of two places in turn, so that a wave that is a scan ahead overwrites none.
+struct Scan {
+  uint64_t (*red)[kDraw / 64];
+  int turn = 0;
+  uint64_t sum = 0;
+  __device__ __forceinline__ uint64_t operator()(uint64_t v) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const uint64_t x = wave_scan_u64(v);
+    if (lane == 63) red[turn][wave] = x;
+    __syncthreads();
+    const uint64_t y = wave_scan_u64(lane < kDraw / 64 ? red[turn][lane] : 0);
+    turn ^= 1;
+    sum = lane_u64(y, 63);
+    return x + (wave ? lane_u64(y, wave - 1) : 0);
   }
-  __syncthreads();
-  return x + sh.red[wave];
-}
+};
 
 struct Row {
   const float* z;
@@ -254,7 +297,7 @@ struct Row {
 // (by count), or the last whose preceding mass is below `want`. Equal logits are
 // cut in id order.
 template <bool BY_MASS>
-__device__ uint64_t search_row(Shared& sh, const Row& r, uint64_t n, double want, uint64_t floor) {
+__device__ uint64_t search_row(Shared& sh, Scan& scan, const Row& r, uint64_t n, double want, uint64_t floor) {
   uint64_t* mass = sh.cand;
   uint32_t* cnt = reinterpret_cast<uint32_t*>(mass + kDigit);
   const int tid = threadIdx.x;
@@ -284,8 +327,8 @@ __device__ uint64_t search_row(Shared& sh, const Row& r, uint64_t n, double want
     const int d0 = D - 1 - 2 * tid, d1 = d0 - 1;
     const uint64_t c0 = d0 >= 0 ? cnt[d0] : 0, c1 = d1 >= 0 ? cnt[d1] : 0;
     const uint64_t m0 = d0 >= 0 ? mass[d0] : 0, m1 = d1 >= 0 ? mass[d1] : 0;
-    const uint64_t cs = above + block_scan(sh, c0 + c1) - c0 - c1;
-    const uint64_t ms = BY_MASS ? above_mass + block_scan(sh, m0 + m1) - m0 - m1 : 0;
+    const uint64_t cs = above + scan(c0 + c1) - c0 - c1;
+    const uint64_t ms = BY_MASS ? above_mass + scan(m0 + m1) - m0 - m1 : 0;
     // the last non-empty digit that starts inside
     auto inside = [&](uint64_t cb, uint64_t mb) { return BY_MASS ? (cb == 0 || (double)mb < want) : cb < n; };
     int last = -1;
@@ -326,9 +369,9 @@ __device__ uint64_t search_row(Shared& sh, const Row& r, uint64_t n, double want
   for (int i0 = 0; i0 < r.V; i0 += kDraw) {
     const int i = i0 + tid;
     const bool is = i < r.V && ordered_bits(clean(r.z[i])) == prefix;
-    const uint64_t x = block_scan(sh, is ? 1 : 0);
+    const uint64_t x = scan(is ? 1 : 0);
     if (is && seen + x == t) sh.key = rank_key(from_ordered_bits(prefix), i);
-    seen += (uint32_t)sh.red[kDraw / 64];
+    seen += (uint32_t)scan.sum;
     if (seen >= t) break;
   }
   __syncthreads();
@@ -340,7 +383,7 @@ __device__ uint64_t search_row(Shared& sh, const Row& r, uint64_t n, double want
 // each) in which the prefix ends, then the keys of that part in order. False:
 // more keys in one part than threads (equal logits).
 template <bool BY_MASS>
-__device__ bool search_bin(Shared& sh, const Row& r, uint32_t N, int bin, uint64_t n, double want, uint64_t above,
+__device__ bool search_bin(Shared& sh, Scan& scan, const Row& r, uint32_t N, int bin, uint64_t n, double want, uint64_t above,
                            uint64_t above_mass, uint64_t floor, uint64_t* key_out, uint64_t* kept_mass) {
   const int tid = threadIdx.x;
   uint64_t* mass = sh.seg;                                       // [kDraw]
@@ -366,8 +409,8 @@ __device__ bool search_bin(Shared& sh, const Row& r, uint32_t N, int bin, uint64
   __syncthreads();
   {
     const uint64_t c0 = cnt[tid], m0 = mass[tid];
-    const uint64_t cb = above + block_scan(sh, c0) - c0;
-    const uint64_t mb = above_mass + block_scan(sh, m0) - m0;
+    const uint64_t cb = above + scan(c0) - c0;
+    const uint64_t mb = above_mass + scan(m0) - m0;
     const bool in = c0 && inside(cb, mb);  // a prefix of the parts
     if (in) atomicMax(&sh.m, (uint32_t)tid);
     __syncthreads();
@@ -397,7 +440,7 @@ __device__ bool search_bin(Shared& sh, const Row& r, uint32_t N, int bin, uint64
   }
   __syncthreads();
   const uint64_t w = tid < (int)m ? by_rank[tid] : 0;
-  const uint64_t x = above_mass + block_scan(sh, w);  // mass through rank tid
+  const uint64_t x = above_mass + scan(w);  // mass through rank tid
   // the ranks inside are a prefix: the last of them
   if (tid < (int)m && inside(above + tid, x - w) && (tid + 1 == (int)m || !inside(above + tid + 1, x))) {
     sh.key = key_by_rank[tid];
@@ -411,8 +454,9 @@ __device__ bool search_bin(Shared& sh, const Row& r, uint32_t N, int bin, uint64
 }
 static_assert(kSegs >= 2 * kDraw, "ranks and their keys fit the segment masses");
 
-__global__ __launch_bounds__(kDraw) void draw_kernel(SampleArgs a, int C) {
+__global__ __launch_bounds__(kDraw) void draw_kernel(SampleArgs a, int C, int chunk) {
   __shared__ Shared sh;
+  Scan scan{sh.red};
   const int row = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const Work w = work_of(a, row, C);
   Row r;
@@ -505,7 +549,7 @@ __global__ __launch_bounds__(kDraw) void draw_kernel(SampleArgs a, int C) {
       // candidates: the first keys of every chunk's list
       uint32_t n = 0;
       if (tid < C) n = w.cnt[(size_t)tid * kBins + deepest];
-      const uint64_t x = block_scan(sh, n);
+      const uint64_t x = scan(n);
       if (tid < C) sh.from[tid] = (uint32_t)(x - n);
       if (tid == C) sh.from[C] = (uint32_t)x;
       __syncthreads();
@@ -529,8 +573,8 @@ __global__ __launch_bounds__(kDraw) void draw_kernel(SampleArgs a, int C) {
     if (by_k) {
       const uint64_t above = k_bin ? sh.cnt[k_bin - 1] : 0, above_mass = k_bin ? sh.mass[k_bin - 1] : 0;
       if (from_list)
-        from_list = search_bin<false>(sh, r, N, k_bin, r.q.k, 0.0, above, above_mass, 0, &r.threshold, &all);
-      if (!from_list) r.threshold = search_row<false>(sh, r, r.q.k, 0.0, 0);
+        from_list = search_bin<false>(sh, scan, r, N, k_bin, r.q.k, 0.0, above, above_mass, 0, &r.threshold, &all);
+      if (!from_list) r.threshold = search_row<false>(sh, scan, r, r.q.k, 0.0, 0);
     }
     if (by_p && !by_bin && !from_list) {
       uint64_t m = 0;
@@ -538,8 +582,8 @@ __global__ __launch_bounds__(kDraw) void draw_kernel(SampleArgs a, int C) {
         const float z = clean(r.z[i]);
         if (z != -INFINITY && rank_key(z, i) >= r.threshold) m += mass_of(exponent_of(z, r.ref, r.q.c));
       }
-      block_scan(sh, m);
-      all = sh.red[kDraw / 64];
+      scan(m);
+      all = scan.sum;
       __syncthreads();
     }
     if (by_p) {
@@ -548,9 +592,9 @@ __global__ __launch_bounds__(kDraw) void draw_kernel(SampleArgs a, int C) {
         const int b = bin_by_mass(want);
         const uint64_t above = b ? sh.cnt[b - 1] : 0, above_mass = b ? sh.mass[b - 1] : 0;
         uint64_t unused;
-        from_list = search_bin<true>(sh, r, N, b, 0, want, above, above_mass, r.threshold, &r.threshold, &unused);
+        from_list = search_bin<true>(sh, scan, r, N, b, 0, want, above, above_mass, r.threshold, &r.threshold, &unused);
       }
-      if (!from_list) r.threshold = search_row<true>(sh, r, 0, want, r.threshold);
+      if (!from_list) r.threshold = search_row<true>(sh, scan, r, 0, want, r.threshold);
     }
     __syncthreads();
     for (int i = tid; i < n_seg; i += kDraw) sh.seg[i] = 0;
@@ -566,25 +610,25 @@ __global__ __launch_bounds__(kDraw) void draw_kernel(SampleArgs a, int C) {
         ++count;
         atomicAdd((unsigned long long*)&sh.seg[key_id(k) / kSeg], (unsigned long long)mass_of(t));
       }
-      block_scan(sh, count);
-      n_kept = (uint32_t)sh.red[kDraw / 64];
+      scan(count);
+      n_kept = (uint32_t)scan.sum;
     }
   } else {
-    // the chunk from the chunks' masses (at most 128 of them)
+    // the chunk from the chunks' masses
     const uint64_t m = tid < C ? w.head[tid].mass : 0;
-    const uint64_t x = block_scan(sh, m);
-    total = sh.red[kDraw / 64];
+    const uint64_t x = scan(m);
+    total = scan.sum;
     const double want = r.q.u * (double)total;
     if (m && (double)x > want && !((double)(x - m) > want)) {
       sh.pick = tid;
       sh.above_mass = x - m;
     }
     __syncthreads();
-    first_seg = (int)sh.pick * (kChunk / kSeg);
-    last_seg = min(n_seg, first_seg + kChunk / kSeg);
+    first_seg = (int)sh.pick * (chunk / kSeg);
+    last_seg = min(n_seg, first_seg + chunk / kSeg);
     before = sh.above_mass;
-    block_scan(sh, tid < C ? w.head[tid].tokens : 0);
-    n_kept = (uint32_t)sh.red[kDraw / 64];
+    scan(tid < C ? w.head[tid].tokens : 0);
+    n_kept = (uint32_t)scan.sum;
     for (int i = tid; i < n_seg; i += kDraw) sh.seg[i] = 0;
     __syncthreads();
   }
@@ -604,8 +648,8 @@ __global__ __launch_bounds__(kDraw) void draw_kernel(SampleArgs a, int C) {
       if (lane == 0) sh.seg[s] = m;
     }
     if (filtered) {
-      block_scan(sh, count);
-      n_kept = (uint32_t)sh.red[kDraw / 64];
+      scan(count);
+      n_kept = (uint32_t)scan.sum;
     }
   }
   __syncthreads();
@@ -613,8 +657,8 @@ __global__ __launch_bounds__(kDraw) void draw_kernel(SampleArgs a, int C) {
   {
     const uint64_t s0 = 2 * tid < n_seg ? sh.seg[2 * tid] : 0;
     const uint64_t s1 = 2 * tid + 1 < n_seg ? sh.seg[2 * tid + 1] : 0;
-    const uint64_t x = before + block_scan(sh, s0 + s1);
-    if (filtered) total = sh.red[kDraw / 64];
+    const uint64_t x = before + scan(s0 + s1);
+    if (filtered) total = scan.sum;
     const double want = r.q.u * (double)total;
     const uint64_t b1 = x - s1, b0 = b1 - s0;
     if (s0 && (double)b1 > want && !((double)b0 > want)) sh.pick = 2 * tid, sh.above_mass = b0;
@@ -626,7 +670,7 @@ __global__ __launch_bounds__(kDraw) void draw_kernel(SampleArgs a, int C) {
   bool kept = false;
   const int id = seg * kSeg + tid;
   const uint64_t m = tid < kSeg && id < r.V ? r.weight(id, kept) : 0;
-  const uint64_t x = c0 + block_scan(sh, m);
+  const uint64_t x = c0 + scan(m);
   const double want = r.q.u * (double)total;
   if (m && (double)x > want && !((double)(x - m) > want)) {
     a.tok[row] = id;
@@ -638,13 +682,23 @@ __global__ __launch_bounds__(kDraw) void draw_kernel(SampleArgs a, int C) {
 
 }  // namespace
 
-size_t sample_row_bytes(int32_t vocab) { return row_bytes(chunks_of(vocab)); }
+// Never falls when an argument grows: fewer rows may take smaller chunks, but then
+// fewer than 4 * 256 in all.
+size_t sample_ws_bytes(int32_t rows, int32_t vocab) {
+  const int64_t few = std::min<int64_t>((int64_t)rows * chunks_of(kFew, vocab), 4 * 256);
+  return std::max(row_bytes(chunks_of(kMany, vocab)) * rows, row_bytes((int)few) + (size_t)16 * rows);
+}
 
 hipError_t launch_sample(const SampleArgs& a, hipStream_t s) {
-  const int C = chunks_of(a.vocab);
-  hipLaunchKernelGGL(top_kernel, dim3(C, a.rows), dim3(kTally), 0, s, a);
-  hipLaunchKernelGGL(tally_kernel, dim3(C, a.rows), dim3(kTally), 0, s, a);
-  hipLaunchKernelGGL(draw_kernel, dim3(a.rows), dim3(kDraw), 0, s, a, C);
+  const int each = each_of(a.rows, a.vocab), C = chunks_of(each, a.vocab);
+  if (each == kFew) {
+    hipLaunchKernelGGL(top_kernel<kFew>, dim3(C, a.rows), dim3(kTally), 0, s, a);
+    hipLaunchKernelGGL(tally_kernel<kFew>, dim3(C, a.rows), dim3(kTally), 0, s, a);
+  } else {
+    hipLaunchKernelGGL(top_kernel<kMany>, dim3(C, a.rows), dim3(kTally), 0, s, a);
+    hipLaunchKernelGGL(tally_kernel<kMany>, dim3(C, a.rows), dim3(kTally), 0, s, a);
+  }
+  hipLaunchKernelGGL(draw_kernel, dim3(a.rows), dim3(kDraw), 0, s, a, C, kTally * each);
   return hipGetLastError();
 }
 

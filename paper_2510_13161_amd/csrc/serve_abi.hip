@@ -221,7 +221,7 @@ msd_status msd_paged_attention(const msd_paged_kv* kv, int32_t layer, const msd_
 
 size_t msd_sample_workspace_bytes(int32_t rows, int32_t vocab) {
   if (rows < 1 || vocab < 1) return 0;
-  return (size_t)rows * sample_row_bytes(vocab);
+  return sample_ws_bytes(rows, vocab);
 }
 
 msd_status msd_sample(const float* logits, int64_t row_stride, int32_t rows, int32_t vocab,

@@ -140,6 +140,13 @@ def test_attention_workspace_never_falls():
                 assert L.msd_paged_attention_workspace_bytes(ctypes.byref(c), batch, n, heads + 4) >= x
 
 
+def test_sample_workspace_never_falls():
+    f = msd.lib().msd_sample_workspace_bytes
+    for rows in (1, 5, 13, 14, 60, 144, 65535):
+        for vocab in (1, 2047, 2049, 8192, 8193, 32000, 152064, 524288, 524289, 1048575):
+            assert 0 < f(rows, vocab) <= f(rows + 1, vocab) and f(rows, vocab) <= f(rows, vocab + 1)
+
+
 @pytest.mark.parametrize("kw,status", [({"logits": None}, -1), ({"u": None}, -1), ({"tok": None}, -1), ({"rows": 0}, -2),
                                        ({"rows": 65536}, -2), ({"vocab": 0}, -2), ({"vocab": 1048577}, -2),
                                        ({"stride": 99}, -2), ({"ws": None}, -5), ({"ws": A + 8}, -5), ({"nb": 0}, -5)])
