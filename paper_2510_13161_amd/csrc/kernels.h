@@ -333,6 +333,7 @@ struct PagedAttnArgs {
                            // chunks share (batch <= kPagedPlanBatch); 0: one a sequence
   float* part_o;           // [wgs][heads][groups][q_per_wg][16][hd]
   float* part_ml;          // [wgs][heads][groups][q_per_wg][16][2]
+  int32_t* plan;           // [batch + 1] chunks of the sequences before each
 };
 constexpr int kPagedMaxTiles = 3;     // query tiles a workgroup holds at most
 constexpr int kPagedPlanBatch = 512;  // sequences whose chunks are planned together at most

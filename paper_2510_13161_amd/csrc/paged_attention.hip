@@ -14,7 +14,6 @@ namespace {
 // of the threads idle at head dim 64).
 template <int HD>
 __global__ __launch_bounds__(256) void paged_merge_kernel(PagedAttnArgs a) {
-  __shared__ int chunk0[kPagedPlanBatch + 1];
   const int tid = threadIdx.x;
   int id = blockIdx.x;
   const int kvh = id % a.kv.heads;
@@ -23,9 +22,7 @@ __global__ __launch_bounds__(256) void paged_merge_kernel(PagedAttnArgs a) {
   const int b = id / (a.groups * a.q_per_wg);
   const int G = a.n_heads / a.kv.heads, Qn = G * a.n_slots;
   if (tile * 16 >= Qn) return;
-  if (tid < 64) plan_chunks(a, chunk0, false);
-  __syncthreads();
-  const int u0 = chunk0[b], nch = chunk0[b + 1] - u0;
+  const int u0 = a.plan[b], nch = a.plan[b + 1] - u0;
   if (nch <= 1) return;  // none, or written by its workgroup
   const int qloc = tid / (HD / 8), c8 = tid % (HD / 8);
   const int qg = tile * 16 + qloc;

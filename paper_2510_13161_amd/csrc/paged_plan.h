@@ -5,38 +5,39 @@
 namespace msd {
 namespace {
 
-// 64-key blocks of a sequence: `sink` of the sinks, [w0, n) from the window on,
-// `own` (0 or 1) of the rows' own keys.
+constexpr int kBlock = 32;  // positions of a block: a wave's share of a round
+constexpr int kWaves = 8;   // waves of a workgroup
+
+// Blocks of a sequence: `sink` of the sinks, [w0, n) from the window on, `own` of
+// the rows' own keys.
 struct Span {
   int sink, w0, n, own;
-  __device__ int total() const { return sink + n - w0 + own; }
+  __device__ int cached() const { return sink + n - w0; }
+  __device__ int total() const { return cached() + own; }
+  __device__ int first_pos(int i) const { return kBlock * (i < sink ? i : i - sink + w0); }
 };
 
 __device__ __forceinline__ int row_count(const PagedAttnArgs& a, int b) {
   return a.count ? min(max(a.count[b], 0), a.n_slots) : a.n_slots;
 }
-__device__ __forceinline__ bool seq_fits(const PagedAttnArgs& a, int b) {
-  const int64_t L = a.kv.len[b];
-  return L >= 0 && L + a.n_slots <= a.kv.capacity;
+__device__ __forceinline__ bool seq_fits(const PagedAttnArgs& a, int len) {
+  return len >= 0 && (int64_t)len + a.n_slots <= a.kv.capacity;
 }
-__device__ __forceinline__ Span seq_span(const PagedAttnArgs& a, int b) {
-  const int cnt = row_count(a, b);
-  if (!seq_fits(a, b) || cnt == 0) return Span{0, 0, 0, 0};
-  const int L = a.kv.len[b];
-  const int end = a.k_new ? L : L + cnt;
+__device__ __forceinline__ Span seq_span(const PagedAttnArgs& a, int len, int cnt) {
+  if (!seq_fits(a, len) || cnt == 0) return Span{0, 0, 0, 0};
+  const int end = a.k_new ? len : len + cnt;
   Span s;
-  s.own = a.k_new ? 1 : 0;
-  s.n = (end + 63) >> 6;
-  s.w0 = a.window > 0 ? min(max(L - a.window + 1, 0) >> 6, s.n) : 0;
-  s.sink = min((int)(((int64_t)a.sinks + 63) >> 6), s.w0);
+  s.own = a.k_new ? (cnt + kBlock - 1) / kBlock : 0;
+  s.n = (end + kBlock - 1) / kBlock;
+  s.w0 = a.window > 0 ? min(max(len - a.window + 1, 0) / kBlock, s.n) : 0;
+  s.sink = (int)min(((int64_t)a.sinks + kBlock - 1) / kBlock, (int64_t)s.w0);
   return s;
 }
 
 // Chunks of G blocks, the same G for every sequence and as small as lets all
 // chunks fit a.wgs workgroups, from the lengths, which only the device knows: one
-// wave tries 64 candidates (multiples of 4, a block for each wave of a
-// workgroup) from an equal share up to one chunk a sequence. chunk0[b] (b <=
-// batch) = chunks of the sequences before b.
+// wave tries 64 candidates (whole rounds of a workgroup) from an equal share up to
+// one chunk a sequence. chunk0[b] (b <= batch) = chunks of the sequences before b.
 __device__ __forceinline__ int plan_chunks(const PagedAttnArgs& a, int* chunk0, bool flag) {
   const int lane = threadIdx.x & 63;
   int total = 0, most = 0;
@@ -44,9 +45,10 @@ __device__ __forceinline__ int plan_chunks(const PagedAttnArgs& a, int* chunk0, 
     const int b = b0 + lane;
     int n = 0;
     if (b < a.batch) {
-      n = seq_span(a, b).total();
+      const int len = a.kv.len[b];
+      n = seq_span(a, len, row_count(a, b)).total();
       chunk0[b] = n;
-      if (flag && !seq_fits(a, b)) atomicOr(a.kv.status, 1u);
+      if (flag && !seq_fits(a, len)) atomicOr(a.kv.status, 1u);
     }
     int t = n, m = n;
 #pragma unroll
@@ -58,11 +60,23 @@ __device__ __forceinline__ int plan_chunks(const PagedAttnArgs& a, int* chunk0, 
     most = max(most, m);
   }
   wave_lds_sync();
-  const int lo = max(4, ((total + a.wgs - 1) / a.wgs + 3) & ~3);
-  const int step = (max(4, (most - lo + 62) / 63) + 3) & ~3;
+  constexpr int R = kWaves - 1;
+  const int lo = max(kWaves, ((total + a.wgs - 1) / a.wgs + R) & ~R);
+  const int step = (max(kWaves, (most - lo + 62) / 63) + R) & ~R;
   const int g = lo + lane * step;  // the last is >= most: one chunk a sequence
   int chunks = 0;
-  for (int b = 0; b < a.batch; ++b) chunks += (chunk0[b] + g - 1) / g;
+  if (most < 1 << 21) {
+    // ceil(n / g) = floor((n - 1/2) / g) + 1, which lies at least 1 / (2 g) from any
+    // integer: the fp32 quotient's error, under n / g * 2^-22, is less than that
+    const float inv = 1.0f / (float)g;
+#pragma unroll 4
+    for (int b = 0; b < a.batch; ++b) {
+      const int n = chunk0[b];
+      chunks += n > 0 ? (int)(((float)n - 0.5f) * inv) + 1 : 0;
+    }
+  } else {
+    for (int b = 0; b < a.batch; ++b) chunks += (chunk0[b] + g - 1) / g;
+  }
   const unsigned long long fit = __ballot(chunks <= a.wgs);
   const int G = lo + step * (fit ? __ffsll((long long)fit) - 1 : 63);
   int before = 0;

@@ -378,13 +378,15 @@ __device__ uint64_t search_row(Shared& sh, Scan& scan, const Row& r, uint64_t n,
   return sh.key;
 }
 
-// The same among the candidate keys >= floor of bin `bin`; `above` tokens and
-// `above_mass` lie in the bins before. First the part of the bin (1024, a thread
-// each) in which the prefix ends, then the keys of that part in order. False:
-// more keys in one part than threads (equal logits).
+// The same among the candidate keys >= floor of bin `bin`, which has `size`;
+// `above` tokens and `above_mass` lie in the bins before. More than kRanked keys
+// are first narrowed to the part of the bin (1024, a thread each) in which the prefix
+// ends; the keys that remain are ranked by counting. False: more of those than
+// threads (equal logits).
+constexpr uint32_t kRanked = 256;
 template <bool BY_MASS>
-__device__ bool search_bin(Shared& sh, Scan& scan, const Row& r, uint32_t N, int bin, uint64_t n, double want, uint64_t above,
-                           uint64_t above_mass, uint64_t floor, uint64_t* key_out, uint64_t* kept_mass) {
+__device__ bool search_bin(Shared& sh, Scan& scan, const Row& r, uint32_t N, int bin, uint32_t size, uint64_t n,
+                           double want, uint64_t above, uint64_t above_mass, uint64_t floor, uint64_t* key_out, uint64_t* kept_mass) {
   const int tid = threadIdx.x;
   uint64_t* mass = sh.seg;                                       // [kDraw]
   uint32_t* cnt = reinterpret_cast<uint32_t*>(sh.seg + kDraw);   // [kDraw]
@@ -393,21 +395,22 @@ __device__ bool search_bin(Shared& sh, Scan& scan, const Row& r, uint32_t N, int
     return bin_of(x) != bin ? -1 : (int)fminf((x - (float)bin) * kDraw, (float)(kDraw - 1));
   };
   auto inside = [&](uint64_t cb, uint64_t mb) { return BY_MASS ? (cb == 0 || (double)mb < want) : cb < n; };
+  int part = -2;  // any
   __syncthreads();
   mass[tid] = 0;
   cnt[tid] = 0;
   if (tid == 0) sh.m = 0, sh.n = 0;
   __syncthreads();
-  for (uint32_t i = tid; i < N; i += kDraw) {
-    const uint64_t k = sh.cand[i];
-    if (k < floor) continue;
-    const int p = part_of(k);
-    if (p < 0) continue;
-    atomicAdd(&cnt[p], 1u);
-    atomicAdd((unsigned long long*)&mass[p], (unsigned long long)r.mass(k));
-  }
-  __syncthreads();
-  {
+  if (size > kRanked) {
+    for (uint32_t i = tid; i < N; i += kDraw) {
+      const uint64_t k = sh.cand[i];
+      if (k < floor) continue;
+      const int p = part_of(k);
+      if (p < 0) continue;
+      atomicAdd(&cnt[p], 1u);
+      atomicAdd((unsigned long long*)&mass[p], (unsigned long long)r.mass(k));
+    }
+    __syncthreads();
     const uint64_t c0 = cnt[tid], m0 = mass[tid];
     const uint64_t cb = above + scan(c0) - c0;
     const uint64_t mb = above_mass + scan(m0) - m0;
@@ -416,20 +419,22 @@ __device__ bool search_bin(Shared& sh, Scan& scan, const Row& r, uint32_t N, int
     __syncthreads();
     if (in && sh.m == (uint32_t)tid) sh.above = cb, sh.above_mass = mb, sh.pick = (uint32_t)c0;
     __syncthreads();
+    part = (int)sh.m;
+    above = sh.above;
+    above_mass = sh.above_mass;
+    if (sh.pick > kDraw) return false;
   }
-  const int part = (int)sh.m;
-  const uint32_t m = sh.pick;
-  above = sh.above;
-  above_mass = sh.above_mass;
-  if (m > kDraw) return false;
   uint64_t* mine = sh.seg;
   for (uint32_t i = tid; i < N; i += kDraw) {
     const uint64_t k = sh.cand[i];
-    if (k >= floor && part_of(k) == part) mine[atomicAdd(&sh.n, 1u)] = k;
+    const int p = part_of(k);
+    if (k >= floor && p >= 0 && (part < 0 || p == part)) mine[atomicAdd(&sh.n, 1u)] = k;
   }
   __syncthreads();
+  const uint32_t m = sh.n;
   const uint64_t key = tid < (int)m ? mine[tid] : 0;
   uint32_t rank = 0;
+#pragma unroll 8
   for (uint32_t i = 0; i < m; ++i) rank += mine[i] > key;
   __syncthreads();
   uint64_t* by_rank = sh.seg;               // masses
@@ -494,9 +499,11 @@ __global__ __launch_bounds__(kDraw) void draw_kernel(SampleArgs a, int C, int ch
       uint32_t n = 0;
       uint64_t m = 0;
       const int b = tid % kBins;
-      for (int c = tid / kBins; c < C; c += kDraw / kBins) {
-        n += w.cnt[(size_t)c * kBins + b];
-        if (by_bin) m += w.mass[(size_t)c * kBins + b];
+#pragma unroll 8
+      for (int c = tid / kBins; c < C; c += kDraw / kBins) n += w.cnt[(size_t)c * kBins + b];
+      if (by_bin) {
+#pragma unroll 4
+        for (int c = tid / kBins; c < C; c += kDraw / kBins) m += w.mass[(size_t)c * kBins + b];
       }
       if (n) atomicAdd(&sh.cnt[b], n);
       if (m) atomicAdd((unsigned long long*)&sh.mass[b], (unsigned long long)m);
@@ -573,7 +580,7 @@ __global__ __launch_bounds__(kDraw) void draw_kernel(SampleArgs a, int C, int ch
     if (by_k) {
       const uint64_t above = k_bin ? sh.cnt[k_bin - 1] : 0, above_mass = k_bin ? sh.mass[k_bin - 1] : 0;
       if (from_list)
-        from_list = search_bin<false>(sh, scan, r, N, k_bin, r.q.k, 0.0, above, above_mass, 0, &r.threshold, &all);
+        from_list = search_bin<false>(sh, scan, r, N, k_bin, (uint32_t)(sh.cnt[k_bin] - above), r.q.k, 0.0, above, above_mass, 0, &r.threshold, &all);
       if (!from_list) r.threshold = search_row<false>(sh, scan, r, r.q.k, 0.0, 0);
     }
     if (by_p && !by_bin && !from_list) {
@@ -592,7 +599,7 @@ __global__ __launch_bounds__(kDraw) void draw_kernel(SampleArgs a, int C, int ch
         const int b = bin_by_mass(want);
         const uint64_t above = b ? sh.cnt[b - 1] : 0, above_mass = b ? sh.mass[b - 1] : 0;
         uint64_t unused;
-        from_list = search_bin<true>(sh, scan, r, N, b, 0, want, above, above_mass, r.threshold, &r.threshold, &unused);
+        from_list = search_bin<true>(sh, scan, r, N, b, (uint32_t)(sh.cnt[b] - above), 0, want, above, above_mass, r.threshold, &r.threshold, &unused);
       }
       if (!from_list) r.threshold = search_row<true>(sh, scan, r, 0, want, r.threshold);
     }

@@ -87,11 +87,12 @@ msd_status fill_append(const msd_paged_kv* kv, const msd_kv_rows* rows, const ms
 
 // Launch shape of an attention call. Query tiles: as few groups as hold them,
 // evenly (each group reads the keys again). Workgroups: where the sequences alone
-// fill fewer than kPagedWgs of them and a sequence can have more blocks than two
-// for each wave, chunks are planned on the device over kPagedWgs workgroups and
-// joined by a second kernel.
-constexpr int64_t kPagedWgs = 256;
-constexpr int64_t kPagedAlone = 8;  // 64-key blocks that one workgroup takes without a split
+// fill fewer than the device holds at once and a sequence can have more blocks
+// than two for each wave, chunks are planned on the device over that many
+// workgroups and joined by a second kernel.
+constexpr int64_t kPagedWgs = 256;    // workgroups in flight of one query tile each (two a compute unit)
+constexpr int64_t kPagedWgsMany = 256;  // of more tiles
+constexpr int64_t kPagedAlone = 16;   // blocks that one workgroup takes without a split
 struct PagedShape {
   int q_per_wg, groups, wgs;
 };
@@ -100,15 +101,16 @@ PagedShape paged_shape(int32_t batch, int32_t n_slots, int32_t n_heads, int32_t 
   PagedShape s;
   s.groups = (tiles + kPagedMaxTiles - 1) / kPagedMaxTiles;
   s.q_per_wg = (tiles + s.groups - 1) / s.groups;
-  const int64_t share = kPagedWgs / ((int64_t)heads * s.groups);
+  const int64_t share = (s.q_per_wg == 1 ? kPagedWgs : kPagedWgsMany) / ((int64_t)heads * s.groups);
   s.wgs = blocks <= kPagedAlone || share <= batch || batch > kPagedPlanBatch
               ? 0
-              : (int)std::min<int64_t>(share, batch * ((blocks + 3) / 4));
+              : (int)std::min<int64_t>(share, batch * ((blocks + 7) / 8));
   return s;
 }
 size_t paged_partials(const PagedShape& s, int32_t heads, int32_t hd) {
   return (size_t)s.wgs * heads * s.groups * s.q_per_wg * 16 * (hd + 2) * sizeof(float);
 }
+constexpr size_t kPagedPlanBytes = (kPagedPlanBatch + 4) * sizeof(int32_t);
 
 }  // namespace
 
@@ -141,12 +143,12 @@ msd_status msd_paged_commit(const msd_paged_kv* kv, const msd_kv_rows* rows, con
 size_t msd_paged_attention_workspace_bytes(const msd_paged_kv* kv, int32_t batch, int32_t n_slots,
                                            int32_t n_heads) {
   if (!kv || batch < 1 || n_slots < 1 || n_heads < 1 || kv->n_kv_heads < 1) return 0;
-  // The most that any smaller call uses: shares of kPagedWgs workgroups of at most
-  // kPagedMaxTiles tiles, of the call's own tiles at most, and at least one
-  // workgroup for each kv head and group.
+  // The most that any smaller call uses: kPagedWgs workgroups of one tile, or
+  // kPagedWgsMany of up to kPagedMaxTiles.
   const size_t tiles = ((size_t)((n_heads + kv->n_kv_heads - 1) / kv->n_kv_heads) * n_slots + 15) / 16;
-  const size_t wgs = (size_t)kPagedWgs;
-  return wgs * std::min<size_t>(tiles, kPagedMaxTiles) * 16 * (kv->head_dim + 2) * sizeof(float) + 16;
+  const size_t most = tiles == 1 ? (size_t)kPagedWgs
+                                 : std::max((size_t)kPagedWgs, (size_t)kPagedWgsMany * std::min<size_t>(tiles, kPagedMaxTiles));
+  return kPagedPlanBytes + most * 16 * (kv->head_dim + 2) * sizeof(float);
 }
 
 msd_status msd_paged_attention(const msd_paged_kv* kv, int32_t layer, const msd_paged_attn* at, void* ws,
@@ -183,17 +185,19 @@ msd_status msd_paged_attention(const msd_paged_kv* kv, int32_t layer, const msd_
       ws_bytes < msd_paged_attention_workspace_bytes(kv, at->batch, at->n_slots, at->n_heads))
     return report(MSD_ERR_WORKSPACE, "workspace NULL, unaligned or too small");
   // blocks that a sequence can have: of its whole capacity, or of the sinks and the window
-  int64_t blocks = (a.kv.capacity + 63) / 64;
+  int64_t blocks = (a.kv.capacity + 31) / 32;
   if (at->window > 0)
-    blocks = std::min(blocks, ((int64_t)at->sinks + 63) / 64 + ((int64_t)at->window + at->n_slots + 62) / 64 + 1);
-  const PagedShape sh = paged_shape(at->batch, at->n_slots, at->n_heads, kv->n_kv_heads, blocks + (at->k_new ? 1 : 0));
+    blocks = std::min(blocks, ((int64_t)at->sinks + 31) / 32 + ((int64_t)at->window + at->n_slots + 30) / 32 + 1);
+  if (at->k_new) blocks += (at->n_slots + 31) / 32;
+  const PagedShape sh = paged_shape(at->batch, at->n_slots, at->n_heads, kv->n_kv_heads, blocks);
   a.q_per_wg = sh.q_per_wg;
   a.groups = sh.groups;
   a.wgs = sh.wgs;
   const size_t rows = (size_t)sh.wgs * kv->n_kv_heads * sh.groups * sh.q_per_wg * 16;
-  a.part_o = static_cast<float*>(ws);
+  a.plan = static_cast<int32_t*>(ws);
+  a.part_o = reinterpret_cast<float*>(static_cast<char*>(ws) + kPagedPlanBytes);
   a.part_ml = a.part_o + rows * kv->head_dim;
-  if (paged_partials(sh, kv->n_kv_heads, kv->head_dim) > ws_bytes)
+  if (kPagedPlanBytes + paged_partials(sh, kv->n_kv_heads, kv->head_dim) > ws_bytes)
     return report(MSD_ERR_WORKSPACE, "workspace too small");
   a.layer = layer;
   a.q = static_cast<const uint16_t*>(at->q);

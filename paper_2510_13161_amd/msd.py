@@ -187,10 +187,11 @@ def _typed(t: torch.Tensor, dtype, shape, what: str) -> torch.Tensor:
 def _fits(kv, rows) -> None:
     """Rows of another head layout than the pages', or tensors of another device than the current one."""
     heads, hd = getattr(rows, "_heads", (None, kv.head_dim))
-    _need(heads in (None, kv.n_kv_heads) and hd == kv.head_dim, "rows and pages differ in kv heads or head_dim")
-    for x in (kv, rows):
-        _need(getattr(x, "_device", torch.cuda.current_device()) == torch.cuda.current_device(),
-              "tensors of another device than the current one")
+    if heads not in (None, kv.n_kv_heads) or hd != kv.head_dim:
+        _need(False, "rows and pages differ in kv heads or head_dim")
+    here = torch.cuda.current_device()
+    if getattr(kv, "_device", here) != here or getattr(rows, "_device", here) != here:
+        _need(False, "tensors of another device than the current one")
 
 
 def _nbytes(ws: torch.Tensor) -> int:
@@ -214,8 +215,8 @@ def _ptr(t: Optional[torch.Tensor]):
 
 
 def _stream(stream) -> Optional[int]:
-    if stream is None:
-        return torch.cuda.current_stream().cuda_stream
+    if stream is None:  # the raw handle: building a Stream object costs more than the call itself
+        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
 
