@@ -335,8 +335,10 @@ struct PagedAttnArgs {
   float* part_ml;          // [wgs][heads][groups][q_per_wg][16][2]
   int32_t* plan;           // [batch + 1] chunks of the sequences before each
 };
-constexpr int kPagedMaxTiles = 3;     // query tiles a workgroup holds at most
-constexpr int kPagedPlanBatch = 512;  // sequences whose chunks are planned together at most
+// Query tiles a workgroup holds at most: 3, and 2 over bf16 pages at head dim 128,
+// whose loads take twice the registers (with 3 it spilled 50).
+constexpr int paged_max_tiles(bool fp8, int head_dim) { return fp8 || head_dim == 64 ? 3 : 2; }
+constexpr int kPagedPlanBatch = 512;  // sequences of a planned call at most
 hipError_t launch_paged_attention(bool fp8, const PagedAttnArgs& a, const Topo& topo, hipStream_t s);
 
 // ---------------------------------------------------------------------------

@@ -6,6 +6,26 @@ namespace msd {
 
 typedef float floatx2 __attribute__((ext_vector_type(2)));
 
+// Inclusive scan of a wave by lane moves inside the vector unit: rows of 16 lanes
+// shifted by 1, 2, 4 and 8, then the last lane of a row given to the next row, and
+// that of the lower half to the upper. Lanes without a source take 0.
+__device__ __forceinline__ int wave_scan_add(int v) {
+  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);
+  return v + __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);
+}
+__device__ __forceinline__ int wave_max_nonneg(int v) {
+  v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, false));
+  v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, false));
+  v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, false));
+  v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, false));
+  v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false));
+  return __builtin_amdgcn_readlane(max(v, __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false)), 63);
+}
+
 // 2^(scale - 127), a biased scale exponent's factor (0 is 2^-127, a subnormal)
 __device__ __forceinline__ float scale_value(uint32_t e) {
   return __uint_as_float(e ? e << 23 : 0x00400000u);

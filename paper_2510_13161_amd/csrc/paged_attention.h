@@ -20,13 +20,9 @@
 //                             row-wise in the wave's LDS and read back by the
 //                             transposing LDS read. Rounding P to one bf16 would
 //                             cost as much as the output's own rounding.
-// A wave loads its next block as soon as the scores have read the keys of the current
-// one, into the same registers. The block's own keys go first, while the first
-// cached block is on its way.
-// The waves are joined in LDS; a chunk that is its sequence's only one writes
-// the output, others leave (max, sum, output) in the workspace and a second
-// kernel joins them in chunk order. No atomics on values: a run repeats bit for
-// bit.
+// The waves are joined in LDS; a chunk that is its sequence's only one writes the
+// output, others leave (max, sum, output) in the workspace and a second kernel
+// joins them in order. No atomics on values: a call repeats bit for bit.
 //
 // Values that no query sees are zeroed as they are staged, so NaN in stale
 // rows, past the window or past the length meets no product. A non-finite value that
@@ -49,12 +45,6 @@ struct Lds {
   static constexpr int kOS = HD + 4;  // floats per row of a wave's output
   static constexpr int kRegion = kBlock * kVS * 2 > 16 * kOS * 4 ? kBlock * kVS * 2 : 16 * kOS * 4;
 };
-
-__device__ __forceinline__ bool finite_bf16(uint32_t b) { return (b & 0x7F80u) != 0x7F80u; }
-// a pair of bf16, non-finite ones as zero
-__device__ __forceinline__ uint32_t finite_pair(uint32_t w) {
-  return (finite_bf16(w) ? w & 0xFFFFu : 0u) | (finite_bf16(w >> 16) ? w & 0xFFFF0000u : 0u);
-}
 
 // 8 codes as bf16, times a power of two
 __device__ __forceinline__ bf16x8 widen8(uint32_t w0, uint32_t w1, float scale) {
@@ -94,6 +84,7 @@ struct Core {
   static constexpr int LPR = HD * EB / 16;                 // lanes of a value row
   static constexpr int VIT = LPR / 2;                      // 16-byte value loads of a block per lane
   static constexpr int KPI = 64 / LPR;                     // value rows of an iteration
+  static constexpr bool kTight = QPW == 1 && HD == 64;  // two workgroups a compute unit
   using L = Lds<HD>;
 
   const PagedAttnArgs a;
@@ -123,38 +114,42 @@ struct Core {
     return pos < end ? a.kv.page_table[(size_t)b * a.kv.max_pages + (pos >> a.kv.page_shift)] : -2;
   }
 
-  __device__ __forceinline__ void load(int k0, int pages) {
+  // where tile t of the block at k0 lies: its first row and its scale
+  __device__ __forceinline__ bool locate(int k0, int pages, int t, size_t& row, size_t& scale) const {
+    int pg = __builtin_amdgcn_readlane(pages, t);
+    const bool ok = pg >= 0 && pg < a.kv.n_pages;
+    if (pg != -2 && !ok && lane == 0) atomicOr(a.kv.status, 8u);
+    pg = ok ? pg : 0;
+    const size_t plane = ((size_t)a.layer * a.kv.n_pages + pg) * a.kv.heads + kvh;
+    const int off = (k0 + 16 * t) & ((1 << a.kv.page_shift) - 1);
+    row = (plane << a.kv.page_shift) + off;
+    scale = row >> 4;  // scales are [..][page / 16]: the plane's and the tile's
+    return ok;
+  }
+  __device__ __forceinline__ void load_keys(int k0, int pages) {
     x0 = k0;
     xvalid = 0;
-    const int mask = (1 << a.kv.page_shift) - 1;
-    const char* kp[2];
-    const char* vp[2];
-    const uint8_t* sp[2];
+    size_t sc[2];
+    const uint32_t at = r16 * (HD * EB) + 16 * g;
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
-      int pg = __builtin_amdgcn_readlane(pages, t);
-      const bool ok = pg >= 0 && pg < a.kv.n_pages;
-      if (pg != -2 && !ok && lane == 0) atomicOr(a.kv.status, 8u);
-      xvalid |= ok ? 1 << t : 0;
-      pg = ok ? pg : 0;
-      const size_t plane = ((size_t)a.layer * a.kv.n_pages + pg) * a.kv.heads + kvh;
-      const int off = (k0 + 16 * t) & mask;
-      const size_t row = (plane << a.kv.page_shift) + off;
-      kp[t] = static_cast<const char*>(a.kv.k) + row * (HD * EB);
-      vp[t] = static_cast<const char*>(a.kv.v) + row * (HD * EB);
-      if (FP8) sp[t] = reinterpret_cast<const uint8_t*>((plane << (a.kv.page_shift - 4)) + (off >> 4));
+      size_t row;
+      xvalid |= locate(k0, pages, t, row, sc[t]) ? 1 << t : 0;
+      const char* p = static_cast<const char*>(a.kv.k) + row * (HD * EB);
+#pragma unroll
+      for (int w = 0; w < KW; ++w) xk[t][w] = *reinterpret_cast<const u32x4*>(p + (at + 64 * w));
     }
-    const uint32_t klane = r16 * (HD * EB) + 16 * g;
+    if (FP8) xscale = (lane & 2 ? a.kv.v_scale : a.kv.k_scale)[lane & 1 ? sc[1] : sc[0]];
+  }
+  __device__ __forceinline__ void load_values(int k0, int pages) {
 #pragma unroll
-    for (int j = 0; j < 2; ++j)
+    for (int t = 0; t < 2; ++t) {
+      size_t row, sc;
+      (void)locate(k0, pages, t, row, sc);
+      const char* p = static_cast<const char*>(a.kv.v) + row * (HD * EB);
 #pragma unroll
-      for (int w = 0; w < KW; ++w) xk[j][w] = *reinterpret_cast<const u32x4*>(kp[j] + (klane + 64 * w));
-#pragma unroll
-    for (int it = 0; it < VIT; ++it)  // an iteration's rows lie in one tile: 16 % KPI = 0
-      xv[it] = *reinterpret_cast<const u32x4*>(vp[it * KPI / 16] + (it * KPI % 16 * (HD * EB) + (uint32_t)lane * 16));
-    if (FP8) {
-      const uint8_t* sc = lane & 2 ? a.kv.v_scale : a.kv.k_scale;
-      xscale = sc[reinterpret_cast<size_t>(lane & 1 ? sp[1] : sp[0])];
+      for (int it = 0; it < VIT / 2; ++it)
+        xv[t * (VIT / 2) + it] = *reinterpret_cast<const u32x4*>(p + ((uint32_t)lane * 16 + 1024 * it));
     }
   }
 
@@ -167,28 +162,29 @@ struct Core {
     return xvalid == 3 && x0 + kBlock <= Len &&
            (a.window <= 0 || pmax - x0 < a.window || x0 + kBlock <= a.sinks);
   }
-  __device__ __forceinline__ bool sees(int t, int pos, int j) const {
-    return ((xvalid >> j) & 1) && pos < end && pos <= pq[t] &&
+  __device__ __forceinline__ bool sees(int t, int pos, int valid, int j) const {
+    return ((valid >> j) & 1) && pos < end && pos <= pq[t] &&
            (a.window <= 0 || pq[t] - pos < a.window || pos < a.sinks);
   }
 
-  // values of the cached block into the wave's LDS; rows that no query sees as zero
-  __device__ __forceinline__ void stage(bool open) {
+  // values of the block at k0 into the wave's LDS (vs0, vs1: its tiles' scales); rows
+  // that no query sees as zero
+  __device__ __forceinline__ void stage(bool open, int k0, int valid, float vs0, float vs1) {
 #pragma unroll
     for (int it = 0; it < VIT; ++it) {
       const int key = it * KPI + lane / LPR;
-      const int t = it * KPI / 16;
+      const int t = it / (VIT / 2);
       u32x4 w = xv[it];
       if (!open) {
-        const int pos = x0 + key;
-        const bool live = ((xvalid >> t) & 1) && pos < end &&
+        const int pos = k0 + key;
+        const bool live = ((valid >> t) & 1) && pos < end &&
                           (a.window <= 0 || Len - pos < a.window || pos < a.sinks);
 #pragma unroll
         for (int i = 0; i < 4; ++i) w[i] = live ? w[i] : 0u;
       }
       uint16_t* dst = vs + key * L::kVS;
       if constexpr (FP8) {
-        const float f = block_scale(2 + t);
+        const float f = t ? vs1 : vs0;
         dst += (lane % LPR) * 16;
         *reinterpret_cast<bf16x8*>(dst) = widen8(w[0], w[1], f);
         *reinterpret_cast<bf16x8*>(dst + 8) = widen8(w[2], w[3], f);
@@ -223,11 +219,9 @@ struct Core {
     }
   }
 
-  // masked scores (base-2 units over s2, -inf where unseen) to the running
-  // softmax and output
-  template <bool CAREFUL>
-  __device__ __forceinline__ void accumulate(floatx4 (&sc)[QPW][2]) {
-    u32x4 ph[QPW], pl[QPW];
+  // masked scores (base-2 units over s2, -inf where unseen) to weights in the running
+  // softmax, in sc and as bf16 hi and lo operands
+  __device__ __forceinline__ void soften(floatx4 (&sc)[QPW][2], u32x4 (&ph)[QPW], u32x4 (&pl)[QPW]) {
 #pragma unroll
     for (int t = 0; t < QPW; ++t) {
       float mx = sc[t][0][0];
@@ -268,6 +262,10 @@ struct Core {
         pl[t][x] = pack_bf16x2(p0 - bf_lo(ph[t][x]), p1 - bf_hi(ph[t][x]));
       }
     }
+  }
+
+  // O += P V over the staged values
+  __device__ __forceinline__ void gather(const u32x4 (&ph)[QPW], const u32x4 (&pl)[QPW]) {
 #pragma unroll
     for (int ds = 0; ds < DSUB; ++ds) {
       // transposing LDS reads: lane takes dim 16 ds + lane % 16 of keys 4 g + e
@@ -275,44 +273,12 @@ struct Core {
       const uint16_t* p0 = vs + (4 * g + (r16 >> 2)) * L::kVS + 16 * ds + 4 * (r16 & 3);
       const v4i16 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16*)p0);
       const v4i16 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16*)(p0 + 16 * L::kVS));
-      u32x4 w = __builtin_bit_cast(u32x4, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
-      if (CAREFUL) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) w[i] = finite_pair(w[i]);
-      }
-      const bf16x8 vb = __builtin_bit_cast(bf16x8, w);
+      const bf16x8 vb = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
 #pragma unroll
       for (int t = 0; t < QPW; ++t) {
         o[t][ds] = mfma16x16x32(__builtin_bit_cast(bf16x8, ph[t]), vb, o[t][ds]);
         o[t][ds] = mfma16x16x32(__builtin_bit_cast(bf16x8, pl[t]), vb, o[t][ds]);
       }
-    }
-    if (CAREFUL) {
-      // the non-finite values, one key after the other, to the queries that
-      // give it weight: query 4 g + r's weight of key 16 j + 4 gk + rk sits in lane
-      // 16 gk + 4 g + r
-#pragma unroll
-      for (int j = 0; j < 2; ++j)
-#pragma unroll
-        for (int rk = 0; rk < 4; ++rk)
-          for (int gk = 0; gk < 4; ++gk) {
-            const uint16_t* row = vs + (16 * j + 4 * gk + rk) * L::kVS + r16;
-            bool any = false;
-#pragma unroll
-            for (int ds = 0; ds < DSUB; ++ds) any |= !finite_bf16(row[16 * ds]);
-            if (!__ballot(any)) continue;
-#pragma unroll
-            for (int t = 0; t < QPW; ++t)
-#pragma unroll
-              for (int r = 0; r < 4; ++r) {
-                const float p = __shfl(sc[t][j][rk], 16 * gk + 4 * g + r);
-#pragma unroll
-                for (int ds = 0; ds < DSUB; ++ds) {
-                  const uint16_t v = row[16 * ds];
-                  if (!finite_bf16(v) && p > 0.0f) o[t][ds][r] += bf2f(v);
-                }
-              }
-          }
     }
   }
 
@@ -335,28 +301,27 @@ struct Core {
     const int k0 = s.first_pos(i0);
     const int first = page_lane(k0);
     if (i0 + kWaves < ic) pages = page_lane(s.first_pos(i0 + kWaves));
-    load(k0, first);
+    load_keys(k0, first);
+    load_values(k0, first);
   }
 
-  template <bool CAREFUL>
   __device__ __forceinline__ void walk(const Span& s, int i0, int i1, int pages) {
     const int ic = min(i1, s.cached());
-    // own blocks of this wave: indices from s.cached() on, congruent to i0
-    for (int i = ic > i0 ? i0 + (ic - i0 + kWaves - 1) / kWaves * kWaves : i0; i < i1; i += kWaves)
-      if (i >= s.cached()) own_block<CAREFUL>((i - s.cached()) * kBlock);
+    floatx4 sc[QPW][2];
+    u32x4 ph[QPW], pl[QPW];
+    if (!kTight) own_blocks(s, i0, ic, i1, sc, ph, pl);
+    // keys of the next block are loaded when the scores have read these, values when
+    // these are staged: either is on its way for most of a round
     for (int i = i0; i < ic; i += kWaves) {
-      const bool open = is_open();
-      // the wave's LDS reads of its previous block are done: one wave's LDS
-      // accesses complete in order
-      wave_lds_sync();
-      stage(open);
-      const float ks0 = block_scale(0), ks1 = block_scale(1);
-      floatx4 sc[QPW][2];
+      const bool open = is_open(), more = i + kWaves < ic;
+      const int k0 = x0, valid = xvalid;
+      const float ks0 = block_scale(0), ks1 = block_scale(1), vs0 = block_scale(2), vs1 = block_scale(3);
       clear(sc);
       scores(sc, [&](int j, int kk) {
         if constexpr (FP8) return widen8(xk[j][kk >> 1][2 * (kk & 1)], xk[j][kk >> 1][2 * (kk & 1) + 1], j ? ks1 : ks0);
         else return __builtin_bit_cast(bf16x8, xk[j][kk]);
       });
+      if (more) load_keys(s.first_pos(i + kWaves), pages);
       if (!open) {
 #pragma unroll
         for (int t = 0; t < QPW; ++t)
@@ -364,15 +329,34 @@ struct Core {
           for (int j = 0; j < 2; ++j)
 #pragma unroll
             for (int r = 0; r < 4; ++r)
-              sc[t][j][r] = sees(t, x0 + 16 * j + 4 * g + r, j) ? sc[t][j][r] : -INFINITY;
+              sc[t][j][r] = sees(t, k0 + 16 * j + 4 * g + r, valid, j) ? sc[t][j][r] : -INFINITY;
       }
-      if (i + kWaves < ic) {
-        load(s.first_pos(i + kWaves), pages);
+      soften(sc, ph, pl);
+      // the wave's LDS reads of its previous block are done: one wave's LDS
+      // accesses complete in order
+      wave_lds_sync();
+      stage(open, k0, valid, vs0, vs1);
+      if (more) {
+        load_values(x0, pages);
         if (i + 2 * kWaves < ic) pages = page_lane(s.first_pos(i + 2 * kWaves));
       }
       wave_lds_sync();
-      accumulate<CAREFUL>(sc);
+      gather(ph, pl);
     }
+    if (kTight) own_blocks(s, i0, ic, i1, sc, ph, pl);
+  }
+
+  // Own blocks of this wave: indices from s.cached() on, congruent to i0. Before the
+  // cached blocks, whose first loads are on their way; with 128 registers a wave
+  // (kTight) after them, when those loads' registers are free.
+  __device__ __forceinline__ void own_blocks(const Span& s, int i0, int ic, int i1, floatx4 (&sc)[QPW][2],
+                                             u32x4 (&ph)[QPW], u32x4 (&pl)[QPW]) {
+    for (int i = ic > i0 ? i0 + (ic - i0 + kWaves - 1) / kWaves * kWaves : i0; i < i1; i += kWaves)
+      if (i >= s.cached()) {
+        own_scores(sc, (i - s.cached()) * kBlock);
+        soften(sc, ph, pl);
+        gather(ph, pl);
+      }
   }
 
   // One row-wise copy in the wave's LDS of the rows' own keys (part 0: rounded to
@@ -382,7 +366,7 @@ struct Core {
     const int64_t seq = b * a.new_seq + kvh * a.new_head;
     const int rows = min(cnt - first, kBlock) * (HD / 8);
     wave_lds_sync();
-#pragma unroll 2
+#pragma unroll 1
     for (int x = lane; x < rows; x += 64) {
       const int key = first + x / (HD / 8), c = x % (HD / 8);
       bf16x8 w;
@@ -403,9 +387,7 @@ struct Core {
   }
 
   // the rows' own keys; rotated ones enter as hi + lo, like the queries
-  template <bool CAREFUL>
-  __device__ __forceinline__ void own_block(int first) {
-    floatx4 sc[QPW][2];
+  __device__ __forceinline__ void own_scores(floatx4 (&sc)[QPW][2], int first) {
     clear(sc);
 #pragma unroll 1
     for (int p = 0; p < QPARTS; ++p) {
@@ -427,7 +409,6 @@ struct Core {
                            (a.window <= 0 || pq[t] - pos < a.window || pos < a.sinks);
           sc[t][j][r] = vis ? sc[t][j][r] : -INFINITY;
         }
-    accumulate<CAREFUL>(sc);
   }
 
   __device__ __forceinline__ bool all_finite() const {
@@ -442,8 +423,114 @@ struct Core {
   }
 };
 
+// The workgroup's chunk once more, a query a wave at a time, in plain steps: two lanes
+// a key for the scores, then a lane the dims lane + 64 i of the keys that the query
+// sees. Only for chunks that hold infinities or NaN.
 template <int HD, bool FP8, int QPW, bool ROT>
-__global__ __launch_bounds__(64 * kWaves, 2) void paged_attn_kernel(PagedAttnArgs a, Topo topo) {
+__device__ __forceinline__ void walk_apart(const Core<HD, FP8, QPW, ROT>& w, const Span& s, int i0, int i1, int qt0,
+                                           int ntile, bool partial, size_t slot0) {
+  using C = Core<HD, FP8, QPW, ROT>;
+  const PagedAttnArgs& a = w.a;
+  const int lane = w.lane, key = lane & 31, half = lane >> 5;
+  const int G = a.n_heads / a.kv.heads, Qn = G * a.n_slots;
+  const int64_t seq = w.b * a.new_seq + w.kvh * a.new_head;
+  auto row_of = [&](int pos) -> int64_t {  // row of the pages, -1: no page
+    const int pg = a.kv.page_table[(size_t)w.b * a.kv.max_pages + (pos >> a.kv.page_shift)];
+    if (pg < 0 || pg >= a.kv.n_pages) return -1;
+    const int64_t plane = ((int64_t)a.layer * a.kv.n_pages + pg) * a.kv.heads + w.kvh;
+    return (plane << a.kv.page_shift) + (pos & ((1 << a.kv.page_shift) - 1));
+  };
+#pragma unroll 1
+  for (int q = threadIdx.x >> 6; q < ntile * 16; q += kWaves) {
+    const int qg = qt0 * 16 + q;
+    if (qg >= Qn) break;
+    int gq, slot;
+    query_of(a, qg, gq, slot);
+    if (slot >= w.cnt) continue;
+    const int P = w.Len + w.depth[slot];
+    const uint64_t anc = w.ancs[slot];
+    float m = -INFINITY, sum = 0.0f, o[HD / 64];
+#pragma unroll
+    for (int i = 0; i < HD / 64; ++i) o[i] = 0.0f;
+#pragma unroll 1
+    for (int i = i0; i < i1; ++i) {
+      const bool own = i >= s.cached();
+      const int k0 = own ? (i - s.cached()) * kBlock : s.first_pos(i);
+      const int at = k0 + key;  // slot or position
+      const int pos = own ? w.Len + w.depth[min(at, kMaxSlots - 1)] : at;
+      bool vis = own ? at < w.cnt && ((anc >> (at & 63)) & 1ull) : at < w.end && at <= P;
+      vis = vis && (a.window <= 0 || P - pos < a.window || pos < a.sinks);
+      const int64_t row = vis && !own ? row_of(at) : 0;
+      vis = vis && row >= 0;
+      float acc = 0.0f;
+      if (vis) {
+#pragma unroll 1
+        for (int c = half * (HD / 16); c < (half + 1) * (HD / 16); ++c) {
+          float k[8];
+          if (own) {
+            load_rotated8(a.k_new + seq + at * a.new_row, c, a.rope, pos, k);
+          } else if constexpr (FP8) {
+            const u32x2 x = *reinterpret_cast<const u32x2*>(static_cast<const uint8_t*>(a.kv.k) + row * HD + 8 * c);
+            const float f = scale_value(a.kv.k_scale[row >> 4]);
+            float lo[4], hi[4];
+            decode4(x[0], lo);
+            decode4(x[1], hi);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) k[e] = lo[e] * f, k[4 + e] = hi[e] * f;
+          } else {
+            load8(static_cast<const uint16_t*>(a.kv.k) + row * HD + 8 * c, k);
+          }
+          int kk, g;
+          operand_place<FP8>(c, kk, g);
+          const uint16_t* qp = w.q_sh + ((((q >> 4) * C::KSTEPS + kk) * C::QPARTS) * 64 + 16 * g + (q & 15)) * 8;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) acc += (bf2f(qp[e]) + (ROT ? bf2f(qp[512 + e]) : 0.0f)) * k[e];
+        }
+      }
+      acc += __shfl_xor(acc, 32);
+      const float sc = vis ? acc * w.s2 : -INFINITY;
+      const float mn = fmaxf(m, wave_max(sc));
+      const float ref = mn == -INFINITY ? 0.0f : mn;
+      const float alpha = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m - ref);
+      const float p = vis ? __builtin_amdgcn_exp2f(sc - ref) : 0.0f;
+      sum = sum * alpha + wave_sum(half ? 0.0f : p);
+      m = mn;
+#pragma unroll
+      for (int e = 0; e < HD / 64; ++e) o[e] *= alpha;
+      const uint32_t seen = (uint32_t)__ballot(vis);
+#pragma unroll 1
+      for (int k = 0; k < kBlock; ++k) {
+        const float pk = __shfl(p, k);
+        if (!((seen >> k) & 1u) || pk == 0.0f) continue;
+        const int64_t r = own ? 0 : row_of(k0 + k);
+#pragma unroll
+        for (int e = 0; e < HD / 64; ++e) {
+          const int d = lane + 64 * e;
+          float v;
+          if (own) v = bf2f(a.v_new[seq + (k0 + k) * a.new_row + d]);
+          else if constexpr (FP8)
+            v = __builtin_amdgcn_cvt_pk_f32_fp8((int)static_cast<const uint8_t*>(a.kv.v)[r * HD + d], false)[0] *
+                scale_value(a.kv.v_scale[r >> 4]);
+          else v = bf2f(static_cast<const uint16_t*>(a.kv.v)[r * HD + d]);
+          o[e] += pk * v;
+        }
+      }
+    }
+    const size_t part = (slot0 * QPW + (q >> 4)) * 16 + (q & 15);
+    if (partial && lane == 0) *reinterpret_cast<float2*>(a.part_ml + part * 2) = make_float2(m, sum);
+    const float inv = sum != 0.0f ? 1.0f / sum : 0.0f;
+#pragma unroll
+    for (int e = 0; e < HD / 64; ++e) {
+      const int d = lane + 64 * e;
+      if (partial) a.part_o[part * HD + d] = o[e];
+      else a.out[w.b * a.out_seq + slot * a.out_row + (w.kvh * G + gq) * a.out_head + d] = f2bf(o[e] * inv);
+    }
+  }
+}
+
+template <int HD, bool FP8, int QPW, bool ROT>
+__global__ __launch_bounds__(64 * kWaves, (Core<HD, FP8, QPW, ROT>::kTight) ? 4 : 2) void paged_attn_kernel(
+    PagedAttnArgs a, Topo topo) {
   using C = Core<HD, FP8, QPW, ROT>;
   using L = Lds<HD>;
   constexpr int kThreads = 64 * kWaves;
@@ -451,7 +538,6 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_attn_kernel(PagedAttnArg
   __shared__ __attribute__((aligned(16))) uint16_t q_sh[QPW * C::KSTEPS * C::QPARTS * 512];
   __shared__ float ml_sh[kWaves][16][2];
   __shared__ int chunk0[kPagedPlanBatch + 1];
-  __shared__ int G_sh;
   __shared__ int depth[kMaxSlots];
   __shared__ uint64_t ancs[kMaxSlots];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -459,26 +545,22 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_attn_kernel(PagedAttnArg
   const int Qn = G * a.n_slots, QT = (Qn + 15) >> 4;
 
   // kv heads first: the hardware deals workgroups to the 8 XCDs in turn, so the
-  // query groups of a chunk that re-read its keys meet in one L2 where the kv
-  // heads are a multiple of 8
+  // query groups of a chunk that re-read its keys meet in one L2 where the kv heads
+  // are a multiple of 8
   int id = blockIdx.x;
   const int kvh = id % a.kv.heads;
   id /= a.kv.heads;
   const int qgi = id % a.groups;
   const int unit = id / a.groups;
-  int b, c = 0, nch = 1;
-  Span s;
-  int i0 = 0, i1;
+  const int qt0 = qgi * QPW, ntile = min(QPW, QT - qt0);
   if (wave == 1) {
     depth[lane] = topo.depth[lane];
     ancs[lane] = topo.anc[lane];
   }
+  if (a.wgs > 0 && wave == 0) plan_chunks(a, chunk0, blockIdx.x == 0);
+  __syncthreads();
+  int b = unit, c = 0, nch = 1;
   if (a.wgs > 0) {
-    if (wave == 0) {
-      const int g = plan_chunks(a, chunk0, blockIdx.x == 0);
-      if (lane == 0) G_sh = g;
-    }
-    __syncthreads();
     if (blockIdx.x == 0)
       for (int i = tid; i <= a.batch; i += kThreads) a.plan[i] = chunk0[i];
     if (unit >= chunk0[a.batch]) return;
@@ -491,20 +573,14 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_attn_kernel(PagedAttnArg
     b = lo;
     c = unit - chunk0[b];
     nch = chunk0[b + 1] - chunk0[b];
-  } else {
-    b = unit;
   }
   const int len = a.kv.len[b], cnt = row_count(a, b);
-  s = seq_span(a, len, cnt);
-  i1 = s.total();
-  if (a.wgs > 0) {
-    i0 = c * G_sh;
-    i1 = min(i1, i0 + G_sh);
-  } else {
-    if (kvh == 0 && qgi == 0 && tid == 0 && !seq_fits(a, len)) atomicOr(a.kv.status, 1u);
-    if (i1 == 0) return;
-    __syncthreads();
-  }
+  const Span s = seq_span(a, len, cnt);
+  if (a.wgs == 0 && kvh == 0 && qgi == 0 && tid == 0 && !seq_fits(a, len)) atomicOr(a.kv.status, 1u);
+  if (s.total() == 0) return;
+  const int size = chunk_size(s.total(), nch);
+  const int i0 = min(c * size, s.total());  // rounding up may leave the last chunks less, or nothing
+  const int i1 = min(s.total(), i0 + size);
 
   C w{a, depth, ancs, q_sh, reinterpret_cast<uint16_t*>(region[wave])};
   w.lane = lane;
@@ -520,7 +596,6 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_attn_kernel(PagedAttnArg
   w.begin(s, i0 + wave, i1, pages);
   // a negative scale turns the queries' sign, so that the largest score is the largest product
   w.s2 = fabsf(a.scale) * kLog2e;
-  const int qt0 = qgi * QPW, ntile = min(QPW, QT - qt0);
 #pragma unroll
   for (int t = 0; t < QPW; ++t) {
     const int qg = (qt0 + t) * 16 + w.r16;
@@ -555,15 +630,14 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_attn_kernel(PagedAttnArg
   }
   __syncthreads();
   w.reset();
-  w.template walk<false>(s, i0 + wave, i1, pages);
-  if (!w.all_finite()) {
-    w.reset();
-    w.begin(s, i0 + wave, i1, pages);
-    w.template walk<true>(s, i0 + wave, i1, pages);
+  w.walk(s, i0 + wave, i1, pages);
+  const size_t slot0 = ((size_t)unit * a.kv.heads + kvh) * a.groups + qgi;  // place of the partial result
+  if (__syncthreads_or(!w.all_finite())) {
+    walk_apart(w, s, i0, i1, qt0, ntile, nch > 1, slot0);
+    return;
   }
 
   // join the waves, tile by tile
-  const size_t slot0 = ((size_t)unit * a.kv.heads + kvh) * a.groups + qgi;  // partial of this workgroup
 #pragma unroll
   for (int t = 0; t < QPW; ++t) {
     if (t >= ntile) break;
@@ -571,7 +645,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_attn_kernel(PagedAttnArg
     float ls = w.lrun[t];
     ls += __shfl_xor(ls, 16);
     ls += __shfl_xor(ls, 32);
-    __syncthreads();
+    if (t) __syncthreads();
 #pragma unroll
     for (int ds = 0; ds < C::DSUB; ++ds)
 #pragma unroll
@@ -619,11 +693,9 @@ void launch_core(const PagedAttnArgs& a, const Topo& topo, dim3 grid, hipStream_
 }
 template <int HD, bool FP8>
 void launch_tiles(const PagedAttnArgs& a, const Topo& topo, dim3 grid, hipStream_t s) {
-  switch (a.q_per_wg) {
-    case 1: return launch_core<HD, FP8, 1>(a, topo, grid, s);
-    case 2: return launch_core<HD, FP8, 2>(a, topo, grid, s);
-    default: return launch_core<HD, FP8, 3>(a, topo, grid, s);
-  }
+  if (a.q_per_wg == 1) return launch_core<HD, FP8, 1>(a, topo, grid, s);
+  if (a.q_per_wg == 2) return launch_core<HD, FP8, 2>(a, topo, grid, s);
+  if constexpr (paged_max_tiles(FP8, HD) == 3) launch_core<HD, FP8, 3>(a, topo, grid, s);
 }
 
 }  // namespace

@@ -90,18 +90,21 @@ msd_status fill_append(const msd_paged_kv* kv, const msd_kv_rows* rows, const ms
 // fill fewer than the device holds at once and a sequence can have more blocks
 // than two for each wave, chunks are planned on the device over that many
 // workgroups and joined by a second kernel.
-constexpr int64_t kPagedWgs = 256;    // workgroups in flight of one query tile each (two a compute unit)
-constexpr int64_t kPagedWgsMany = 256;  // of more tiles
+constexpr int64_t kPagedWgs = 512;    // workgroups of one query tile at head dim 64 (two fit a compute unit)
+constexpr int64_t kPagedWgsMany = 256;  // others (one fits)
 constexpr int64_t kPagedAlone = 16;   // blocks that one workgroup takes without a split
 struct PagedShape {
   int q_per_wg, groups, wgs;
 };
-PagedShape paged_shape(int32_t batch, int32_t n_slots, int32_t n_heads, int32_t heads, int64_t blocks) {
+PagedShape paged_shape(const msd_paged_kv* kv, int32_t batch, int32_t n_slots, int32_t n_heads, int64_t blocks) {
+  const int32_t heads = kv->n_kv_heads;
+  const bool light = kv->head_dim == 64;
   const int tiles = (n_heads / heads * n_slots + 15) / 16;
   PagedShape s;
-  s.groups = (tiles + kPagedMaxTiles - 1) / kPagedMaxTiles;
+  const int most = paged_max_tiles(kv->format == MSD_KV_FP8, kv->head_dim);
+  s.groups = (tiles + most - 1) / most;
   s.q_per_wg = (tiles + s.groups - 1) / s.groups;
-  const int64_t share = (s.q_per_wg == 1 ? kPagedWgs : kPagedWgsMany) / ((int64_t)heads * s.groups);
+  const int64_t share = (s.q_per_wg == 1 && light ? kPagedWgs : kPagedWgsMany) / ((int64_t)heads * s.groups);
   s.wgs = blocks <= kPagedAlone || share <= batch || batch > kPagedPlanBatch
               ? 0
               : (int)std::min<int64_t>(share, batch * ((blocks + 7) / 8));
@@ -144,10 +147,10 @@ size_t msd_paged_attention_workspace_bytes(const msd_paged_kv* kv, int32_t batch
                                            int32_t n_heads) {
   if (!kv || batch < 1 || n_slots < 1 || n_heads < 1 || kv->n_kv_heads < 1) return 0;
   // The most that any smaller call uses: kPagedWgs workgroups of one tile, or
-  // kPagedWgsMany of up to kPagedMaxTiles.
+  // kPagedWgsMany of up to 3.
   const size_t tiles = ((size_t)((n_heads + kv->n_kv_heads - 1) / kv->n_kv_heads) * n_slots + 15) / 16;
   const size_t most = tiles == 1 ? (size_t)kPagedWgs
-                                 : std::max((size_t)kPagedWgs, (size_t)kPagedWgsMany * std::min<size_t>(tiles, kPagedMaxTiles));
+                                 : std::max((size_t)kPagedWgs, (size_t)kPagedWgsMany * std::min<size_t>(tiles, 3));
   return kPagedPlanBytes + most * 16 * (kv->head_dim + 2) * sizeof(float);
 }
 
@@ -189,7 +192,7 @@ msd_status msd_paged_attention(const msd_paged_kv* kv, int32_t layer, const msd_
   if (at->window > 0)
     blocks = std::min(blocks, ((int64_t)at->sinks + 31) / 32 + ((int64_t)at->window + at->n_slots + 30) / 32 + 1);
   if (at->k_new) blocks += (at->n_slots + 31) / 32;
-  const PagedShape sh = paged_shape(at->batch, at->n_slots, at->n_heads, kv->n_kv_heads, blocks);
+  const PagedShape sh = paged_shape(kv, at->batch, at->n_slots, at->n_heads, blocks);
   a.q_per_wg = sh.q_per_wg;
   a.groups = sh.groups;
   a.wgs = sh.wgs;
