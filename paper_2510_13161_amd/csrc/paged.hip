@@ -27,66 +27,117 @@ __device__ __forceinline__ int append_count(const AppendArgs& a, int b, int64_t 
   return *bad_capacity ? 0 : n;
 }
 
+// The 8 dims of a row that a lane holds, as two groups of 4: of rotated keys in the
+// half layout the two halves of 4 pairs (no lane needs another's dims, and a pair's
+// (cos, sin) is read once), else 8 in a row.
+struct Dims {
+  int d0, d1;
+  bool turned;
+};
+__device__ __forceinline__ Dims dims_of(int c, const RopeView& rp) {
+  if (rp.table && 8 * c < rp.rd) {
+    if (rp.interleaved) return {8 * c, 8 * c + 4, true};
+    return {4 * c, rp.rd / 2 + 4 * c, true};
+  }
+  return {8 * c, 8 * c + 4, false};
+}
+__device__ __forceinline__ void unpack4(u32x2 w, float* v) {
+  v[0] = bf_lo(w[0]);
+  v[1] = bf_hi(w[0]);
+  v[2] = bf_lo(w[1]);
+  v[3] = bf_hi(w[1]);
+}
+// Rotates a lane's 4 pairs by their table entries: each product and difference
+// rounded by itself, as load_rotated8 does.
+__device__ __forceinline__ void turn(float (&v)[8], const float2* cs, bool interleaved) {
+#pragma clang fp contract(off)
+  float2 f[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) f[i] = cs[i];
+  if (interleaved) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float a = v[2 * i], b = v[2 * i + 1];
+      v[2 * i] = a * f[i].x - b * f[i].y;
+      v[2 * i + 1] = b * f[i].x + a * f[i].y;
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float a = v[i], b = v[4 + i];
+      v[i] = a * f[i].x - b * f[i].y;
+      v[4 + i] = b * f[i].x + a * f[i].y;
+    }
+  }
+}
+
 template <int HD, bool FP8>
 __global__ __launch_bounds__(256) void append_kernel(AppendArgs a, int n_blocks) {
-  constexpr int C8 = HD / 8;        // 8-dim groups of a row
+  constexpr int C8 = HD / 8;        // lanes of a row
   constexpr int RPI = 64 / C8;      // rows of an iteration
   constexpr int IT = 16 / RPI;      // iterations of a block
   const int lane = threadIdx.x & 63;
-  int64_t item = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  const int which = (int)(item & 1);  // 0 keys, 1 values
-  item >>= 1;
-  const int h = (int)(item % a.kv.heads);
-  item /= a.kv.heads;
-  const int j = (int)(item % n_blocks);
-  item /= n_blocks;
-  const int b = (int)(item % a.batch);
-  const int l = (int)(item / a.batch);
-  if (l >= a.n_layers) return;
+  const int item = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6));
+  const int which = item & 1;  // 0 keys, 1 values
+  const int h = (item >> 1) % a.kv.heads, j = (item >> 1) / a.kv.heads;
+  const int b = blockIdx.y, l = blockIdx.z;
+  if (j >= n_blocks) return;
   const int64_t L = a.kv.len[b];
   bool bad;
   const int n = append_count(a, b, L, &bad);
-  if (bad && j == 0 && h == 0 && which == 0 && l == 0 && lane == 0) atomicOr(a.kv.status, 1u);
+  if (bad && item == 0 && l == 0 && lane == 0) atomicOr(a.kv.status, 1u);
   if (n == 0) return;
   const int64_t t0 = (L / kScaleTokens + j) * kScaleTokens;  // first position of the block
   if (t0 >= L + n) return;
-  const int page = a.kv.page_table[(size_t)b * a.kv.max_pages + (size_t)(t0 >> a.kv.page_shift)];
-  if (page < 0 || page >= a.kv.n_pages) {
-    if (h == 0 && which == 0 && l == 0 && lane == 0) atomicOr(a.kv.status, 8u);
-    return;
-  }
-  const int page_size = 1 << a.kv.page_shift;
-  const int off = (int)(t0 & (page_size - 1));
-  const size_t plane = ((size_t)(a.layer + l) * a.kv.n_pages + page) * a.kv.heads + h;
-  const size_t row0 = (plane * page_size + off) * HD;  // first element of the block
-  const uint16_t* src = (which ? a.v : a.k) + l * a.layer_stride + b * a.seq_stride + h * a.head_stride;
+  const int c = lane % C8, rl = lane / C8;
   const RopeView rp = which ? RopeView{nullptr, 0, 0} : a.rope;
-  const int c = lane % C8;
+  const Dims d = dims_of(c, rp);
 
-  // new rows of this lane, fp32
-  float x[IT][8];
+  // the page's number and the rows are on their way together, then the block's scale
+  const int page = a.kv.page_table[(size_t)b * a.kv.max_pages + (size_t)(t0 >> a.kv.page_shift)];
+  const uint16_t* src = (which ? a.v : a.k) + l * a.layer_stride + b * a.seq_stride + h * a.head_stride;
+  const int first = (int)(t0 - L);  // row of the block's first place, negative where it is held
   bool now[IT];
+  float x[IT][8];
 #pragma unroll
   for (int it = 0; it < IT; ++it) {
-    const int64_t pos = t0 + it * RPI + lane / C8;
-    now[it] = pos >= L && pos < L + n;
+    int r = first + it * RPI + rl;
+    now[it] = r >= 0 && r < n;
 #pragma unroll
     for (int i = 0; i < 8; ++i) x[it][i] = 0.0f;
     if (now[it]) {
-      int r = (int)(pos - L);
+      const int64_t pos = L + r;
       if (a.path) r = min(max(a.path[(size_t)b * a.n_rows + r], 0), a.n_rows - 1);
-      load_rotated8(src + r * a.row_stride, c, rp, pos, x[it]);
+      const uint16_t* row = src + r * a.row_stride;
+      unpack4(*reinterpret_cast<const u32x2*>(row + d.d0), x[it]);
+      unpack4(*reinterpret_cast<const u32x2*>(row + d.d1), x[it] + 4);
+      if (d.turned) turn(x[it], rp.table + pos * (rp.rd / 2) + 4 * c, rp.interleaved != 0);
     }
   }
+  const bool paged = page >= 0 && page < a.kv.n_pages;
+  const size_t plane = ((size_t)(a.layer + l) * a.kv.n_pages + (paged ? page : 0)) * a.kv.heads + h;
+  const size_t row0 = (plane << a.kv.page_shift) + (size_t)(t0 & ((1 << a.kv.page_shift) - 1));  // first row of the block
+  const bool held = first < 0;  // committed rows in the block
+  uint8_t* sc = (which ? a.kv.v_scale : a.kv.k_scale) + (row0 >> 4);
+  const uint32_t was = FP8 && held ? *sc : 0;
+  if (!paged) {
+    if (h == 0 && which == 0 && l == 0 && lane == 0) atomicOr(a.kv.status, 8u);
+    return;
+  }
+
   if constexpr (!FP8) {
-    uint16_t* dst = static_cast<uint16_t*>(which ? a.kv.v : a.kv.k) + row0;
+    uint16_t* dst = static_cast<uint16_t*>(which ? a.kv.v : a.kv.k) + row0 * HD;
 #pragma unroll
     for (int it = 0; it < IT; ++it)
-      if (now[it])
-        *reinterpret_cast<bf16x8*>(dst + (it * RPI + lane / C8) * HD + 8 * c) = round_vals(x[it]);
+      if (now[it]) {
+        uint16_t* at = dst + (it * RPI + rl) * HD;
+        const u32x2 lo = {pack_bf16x2(x[it][0], x[it][1]), pack_bf16x2(x[it][2], x[it][3])};
+        const u32x2 hi = {pack_bf16x2(x[it][4], x[it][5]), pack_bf16x2(x[it][6], x[it][7])};
+        *reinterpret_cast<u32x2*>(at + d.d0) = lo;
+        *reinterpret_cast<u32x2*>(at + d.d1) = hi;
+      }
   } else {
-    uint8_t* dst = static_cast<uint8_t*>(which ? a.kv.v : a.kv.k) + row0;
-    uint8_t* sc = (which ? a.kv.v_scale : a.kv.k_scale) + plane * (page_size / kScaleTokens) + off / kScaleTokens;
+    uint8_t* dst = static_cast<uint8_t*>(which ? a.kv.v : a.kv.k) + row0 * HD;
     float amax = 0.0f;
 #pragma unroll
     for (int it = 0; it < IT; ++it)
@@ -96,29 +147,27 @@ __global__ __launch_bounds__(256) void append_kernel(AppendArgs a, int n_blocks)
         amax = m <= 3.402823466e38f ? fmaxf(amax, m) : amax;  // infinities and NaN left out
       }
     amax = wave_max(amax);
-    const uint32_t was = *sc;
-    const bool held = t0 < L;  // committed rows in the block
-    uint32_t e = scale_exponent(amax);
-    if (held) e = max(e, was);
+    const uint32_t e = max(scale_exponent(amax), was);
     const float inv = __uint_as_float(e < 254u ? (254u - e) << 23 : 0x00400000u);  // 2^(127 - e)
 #pragma unroll
     for (int it = 0; it < IT; ++it) {
-      u32x2* at = reinterpret_cast<u32x2*>(dst + (it * RPI + lane / C8) * HD + 8 * c);
+      uint8_t* at = dst + (it * RPI + rl) * HD;
       if (now[it]) {
         float y[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) y[i] = clamp_code(x[it][i] * inv);
-        *at = u32x2{encode4(y[0], y[1], y[2], y[3]), encode4(y[4], y[5], y[6], y[7])};
-      } else if (held && e > was && t0 + it * RPI + lane / C8 < L) {
+        *reinterpret_cast<uint32_t*>(at + d.d0) = encode4(y[0], y[1], y[2], y[3]);
+        *reinterpret_cast<uint32_t*>(at + d.d1) = encode4(y[4], y[5], y[6], y[7]);
+      } else if (held && e > was && first + it * RPI + rl < 0) {
         const float f = exp2_int((int)was - (int)e);
-        u32x2 w = *at;
+        u32x2 w = *reinterpret_cast<u32x2*>(at + 8 * c);
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
           float y[4];
           decode4(w[i], y);
           w[i] = encode4(y[0] * f, y[1] * f, y[2] * f, y[3] * f);
         }
-        *at = w;
+        *reinterpret_cast<u32x2*>(at + 8 * c) = w;
       }
     }
     if (lane == 0) *sc = (uint8_t)e;
@@ -136,10 +185,7 @@ __global__ void advance_kernel(AppendArgs a) {
 
 hipError_t launch_paged_append(bool fp8, const AppendArgs& a, hipStream_t s) {
   const int n_blocks = (a.n_rows + 14) / 16 + 1;  // n rows touch that many 16-token blocks at most
-  const int64_t waves = (int64_t)a.n_layers * a.batch * n_blocks * a.kv.heads * 2;
-  const int64_t wgs = (waves + 3) / 4;
-  if (wgs > 0x7FFFFFFF / 256) return hipErrorInvalidValue;
-  const dim3 grid((uint32_t)wgs), block(256);
+  const dim3 grid((uint32_t)(((int64_t)n_blocks * a.kv.heads + 1) / 2), a.batch, a.n_layers), block(256);
   if (a.kv.head_dim == 128) {
     if (fp8) hipLaunchKernelGGL((append_kernel<128, true>), grid, block, 0, s, a, n_blocks);
     else hipLaunchKernelGGL((append_kernel<128, false>), grid, block, 0, s, a, n_blocks);

@@ -79,9 +79,10 @@ msd_status fill_append(const msd_paged_kv* kv, const msd_kv_rows* rows, const ms
   a->batch = rows->batch;
   a->n_rows = rows->n_rows;
   a->count = rows->count;
-  // a wave for every (layer, sequence, block, head) of k and of v
-  const int64_t waves = (int64_t)a->n_layers * a->batch * ((a->n_rows + 14) / 16 + 1);
-  if (waves > ((int64_t)1 << 31) / 64 / (2 * a->kv.heads)) return report(MSD_ERR_SHAPE, "too many rows for one call");
+  // the grid: blocks and heads, sequences, layers
+  if (a->batch > 65535 || a->n_layers > 65535 ||
+      (int64_t)((a->n_rows + 14) / 16 + 1) * a->kv.heads > (int64_t)1 << 24)
+    return report(MSD_ERR_SHAPE, "too many rows for one call");
   return MSD_OK;
 }
 
