@@ -28,6 +28,7 @@
  *   msd_paged_commit     the accepted path of a block into it (Sec. 2 commit);
  *   msd_paged_attention  attention of a block's rows over it, with a sliding
  *                        window and sinks;
+ *   msd_verify_block_paged  the verification pass over such a cache;
  *   msd_sample           tokens under temperature, top-k, top-p and min-p.
  *
  * Conventions
@@ -521,6 +522,26 @@ size_t msd_paged_attention_workspace_bytes(const msd_paged_kv* kv, int32_t batch
                                            int32_t n_heads);
 msd_status msd_paged_attention(const msd_paged_kv* kv, int32_t layer, const msd_paged_attn* attn,
                                void* ws, size_t ws_bytes, hipStream_t stream);
+
+/*
+ * msd_verify_block over a paged cache: the committed positions are read from
+ * its pages (all layers; n_layers, n_kv_heads and head_dim the model's,
+ * max_pages * page_size at most max_positions), and the block's own keys and
+ * values, rotated as the model does, go to k_rows and v_rows, device bf16
+ * [n_layers][batch][n_kv_heads][n_slots][head_dim], 16-byte aligned: no page
+ * holds a draft before msd_paged_commit stores the accepted ones (rope NULL,
+ * strides of that layout). window and sinks as in msd_paged_attn, in every
+ * layer. Outputs and limits of msd_verify_block; the cached keys of an 8-bit
+ * cache enter as the values they stand for. ws of
+ * msd_verify_paged_workspace_bytes (it never falls when batch, n_slots or
+ * kappa grows), 16-byte aligned.
+ */
+size_t msd_verify_paged_workspace_bytes(const msd_model* model, const msd_paged_kv* kv, int32_t batch,
+                                        int32_t n_slots, int32_t kappa);
+msd_status msd_verify_block_paged(const msd_model* model, const msd_paged_kv* kv, const msd_block* block,
+                                  const msd_ee_request* ee, void* k_rows, void* v_rows, int32_t window,
+                                  int32_t sinks, float* logits, int32_t* argmax, float* lse, void* ws,
+                                  size_t ws_bytes, hipStream_t stream);
 
 /*
  * Tokens from rows of logits, one uniform each. Per row, in this order:

@@ -452,7 +452,7 @@ __device__ void epi_qkv(const GemmArgs& a, int t, int mt, const floatx4 (&acc)[J
   if (m >= a.M) return;
   const int b = m / a.n_slots, slot = m - b * a.n_slots;
   const int L = in.L;
-  if (L < 0 || L + a.n_slots > a.capacity) {
+  if (L < 0 || (int64_t)L + a.n_slots > a.positions) {
     if (q == 0 && slot == 0) atomicOr(a.status, 1u);
     return;
   }
@@ -501,7 +501,7 @@ __device__ void epi_qkv(const GemmArgs& a, int t, int mt, const floatx4 (&acc)[J
       }
     } else {
       uint16_t* cache = which == 1 ? a.k_cache : a.v_cache;
-      uint16_t* row = cache + (((size_t)b * Hk + hloc) * a.capacity + L + slot) * hd;
+      uint16_t* row = cache + (((size_t)b * Hk + hloc) * a.capacity + (a.beside ? 0 : L) + slot) * hd;
       const u32x2 wl = {pack_bf16x2(lo[0], lo[1]), pack_bf16x2(lo[2], lo[3])};
       const u32x2 wh = {pack_bf16x2(hi[0], hi[1]), pack_bf16x2(hi[2], hi[3])};
       *reinterpret_cast<u32x2*>(row + dlo) = wl;

@@ -94,6 +94,9 @@ struct GemmArgs {
   const int32_t* len;      // committed lengths [batch]
   uint32_t* status;
   int32_t capacity, n_slots;
+  int32_t beside;          // 1: the block's rows go to rows 0 .. n_slots-1 of a buffer of
+                           // `capacity` rows beside the cache, else to len + slot
+  int64_t positions;       // positions a sequence can have (the cache's capacity)
   const float2* rope;      // [max_positions][hd/2] (cos, sin), or null
   int32_t rope_rows;
   int32_t depth[kMaxSlots];
@@ -322,6 +325,11 @@ struct PagedAttnArgs {
   int64_t q_seq, q_row, q_head;
   uint16_t* out;
   int64_t out_seq, out_row, out_head;
+  // a verify pass: queries from the QKV epilogue's operand image, output into the
+  // output projection's image (null: q and out)
+  const uint16_t* q_img;   // GemmArgs::q_img
+  uint16_t* out_img;       // activation image, MT row tiles
+  int32_t MT;
   const uint16_t* k_new;   // or null: the block's rows are in the pages
   const uint16_t* v_new;
   int64_t new_seq, new_row, new_head;

@@ -284,9 +284,19 @@ msd_status static_scratch_address(void** out) {
 
 msd_status verify_prepare(const msd_model* m, msd_kv_cache* kv, const msd_block* blk,
                           const msd_ee_request* ee, const int32_t* argmax, Topo* topo, Layout* Lout);
+// A verify pass over a paged cache: kv then describes the buffers that take the
+// block's own keys and values ([layers][batch][kv heads][n_slots][head_dim]).
+struct PagedPass {
+  const msd_paged_kv* kv;
+  PagedView view;
+  int32_t window, sinks;
+  void* ws;          // the attention's workspace
+  size_t ws_bytes;
+};
 msd_status verify_launch(const msd_model* m, msd_kv_cache* kv, const msd_block* blk,
                          const msd_ee_request* ee, float* logits, int32_t* argmax, float* lse,
-                         char* w, const Topo& topo, const Layout& L, hipStream_t stream);
+                         char* w, const Topo& topo, const Layout& L, hipStream_t stream,
+                         const PagedPass* paged = nullptr);
 
 }  // namespace
 
@@ -632,7 +642,8 @@ msd_status verify_prepare(const msd_model* m, msd_kv_cache* kv, const msd_block*
 // head, all on `stream`, using the workspace at w laid out as L.
 msd_status verify_launch(const msd_model* m, msd_kv_cache* kv, const msd_block* blk,
                          const msd_ee_request* ee, float* logits, int32_t* argmax, float* lse,
-                         char* w, const Topo& topo, const Layout& L, hipStream_t stream) {
+                         char* w, const Topo& topo, const Layout& L, hipStream_t stream,
+                         const PagedPass* paged) {
   msd_status st = MSD_OK;
   const msd_model_config& c = m->cfg;
   const int M = blk->batch * blk->n_slots;
@@ -697,41 +708,67 @@ msd_status verify_launch(const msd_model* m, msd_kv_cache* kv, const msd_block* 
     g.status = kv->status;
     g.capacity = kv->capacity;
     g.n_slots = blk->n_slots;
+    g.beside = paged ? 1 : 0;
+    g.positions = paged ? paged->view.capacity : kv->capacity;
     g.rope = m->rope;
     g.rope_rows = c.max_positions;
     for (int i = 0; i < kMaxSlots; ++i) g.depth[i] = topo.depth[i];
     MSD_HIP(launch_gemm(EPI_QKV, g, stream, prof_events(m, MSD_K_QKV, l)));
 
-    AttnArgs aa{};
-    aa.q_img = q_img;
-    aa.k_cache = kc;
-    aa.v_cache = vc;
-    aa.len = kv->len;
-    aa.status = kv->status;
-    aa.out_img = img_attn;
-    aa.MT = L.MT;
-    aa.counters = counters + L.n_gemm_counters;
-    aa.part_o = reinterpret_cast<float*>(w + L.part_o);
-    aa.part_ml = reinterpret_cast<float*>(w + L.part_ml);
-    aa.batch = blk->batch;
-    aa.n_heads = c.n_heads;
-    aa.n_kv_heads = c.n_kv_heads;
-    aa.capacity = kv->capacity;
-    aa.n_slots = blk->n_slots;
-    aa.max_chunks = L.max_chunks;
-    const AttnShape ash = attn_shape(m, L.max_chunks, c.n_kv_heads, blk->batch, q_tiles, c.head_dim);
-    aa.q_per_wg = ash.q_per_wg;
-    aa.nb = ash.nb;
-    aa.ring = ash.ring ? 1 : 0;
-    aa.wgs = ash.wgs;
-    aa.chunk_blocks = ash.chunk_blocks;
-    aa.scale = 1.0f / std::sqrt((float)c.head_dim);
-    aa.topo = topo;
-    aa.defer = attn_defer(m, L.max_chunks, blk->batch, ash) ? 1 : 0;
-    MSD_HIP(prof_mark(m, MSD_K_ATTN, l, true, stream));
-    MSD_HIP(launch_attention(c.head_dim, aa, stream));
-    if (aa.defer) MSD_HIP(launch_attention_merge(c.head_dim, aa, stream));
-    MSD_HIP(prof_mark(m, MSD_K_ATTN, l, false, stream));
+    if (paged) {
+      PagedAttnArgs pa{};
+      pa.kv = paged->view;
+      pa.layer = l;
+      pa.q_img = q_img;
+      pa.out_img = img_attn;
+      pa.MT = L.MT;
+      pa.k_new = kc;
+      pa.v_new = vc;
+      pa.new_row = c.head_dim;
+      pa.new_head = (int64_t)kv->capacity * c.head_dim;
+      pa.new_seq = (int64_t)c.n_kv_heads * pa.new_head;
+      pa.scale = 1.0f / std::sqrt((float)c.head_dim);
+      pa.batch = blk->batch;
+      pa.n_slots = blk->n_slots;
+      pa.n_heads = c.n_heads;
+      pa.window = paged->window;
+      pa.sinks = paged->sinks;
+      MSD_HIP(prof_mark(m, MSD_K_ATTN, l, true, stream));
+      st = run_paged_attention(paged->kv, pa, topo, paged->ws, paged->ws_bytes, stream);
+      if (st != MSD_OK) return st;
+      MSD_HIP(prof_mark(m, MSD_K_ATTN, l, false, stream));
+    } else {
+      AttnArgs aa{};
+      aa.q_img = q_img;
+      aa.k_cache = kc;
+      aa.v_cache = vc;
+      aa.len = kv->len;
+      aa.status = kv->status;
+      aa.out_img = img_attn;
+      aa.MT = L.MT;
+      aa.counters = counters + L.n_gemm_counters;
+      aa.part_o = reinterpret_cast<float*>(w + L.part_o);
+      aa.part_ml = reinterpret_cast<float*>(w + L.part_ml);
+      aa.batch = blk->batch;
+      aa.n_heads = c.n_heads;
+      aa.n_kv_heads = c.n_kv_heads;
+      aa.capacity = kv->capacity;
+      aa.n_slots = blk->n_slots;
+      aa.max_chunks = L.max_chunks;
+      const AttnShape ash = attn_shape(m, L.max_chunks, c.n_kv_heads, blk->batch, q_tiles, c.head_dim);
+      aa.q_per_wg = ash.q_per_wg;
+      aa.nb = ash.nb;
+      aa.ring = ash.ring ? 1 : 0;
+      aa.wgs = ash.wgs;
+      aa.chunk_blocks = ash.chunk_blocks;
+      aa.scale = 1.0f / std::sqrt((float)c.head_dim);
+      aa.topo = topo;
+      aa.defer = attn_defer(m, L.max_chunks, blk->batch, ash) ? 1 : 0;
+      MSD_HIP(prof_mark(m, MSD_K_ATTN, l, true, stream));
+      MSD_HIP(launch_attention(c.head_dim, aa, stream));
+      if (aa.defer) MSD_HIP(launch_attention_merge(c.head_dim, aa, stream));
+      MSD_HIP(prof_mark(m, MSD_K_ATTN, l, false, stream));
+    }
 
     g = gemm_base(m, L, w, M, s.o, d);
     g.a_img = img_attn;
@@ -784,6 +821,44 @@ msd_status verify_launch(const msd_model* m, msd_kv_cache* kv, const msd_block* 
 }  // namespace
 
 extern "C" {
+
+size_t msd_verify_paged_workspace_bytes(const msd_model* m, const msd_paged_kv* kv, int32_t batch, int32_t n_slots,
+                                        int32_t kappa) {
+  if (!m || !kv || batch < 1 || n_slots < 1) return 0;
+  return layout(m, batch, n_slots, kappa, n_slots).total +
+         msd_paged_attention_workspace_bytes(kv, batch, n_slots, m->cfg.n_heads);
+}
+
+msd_status msd_verify_block_paged(const msd_model* m, const msd_paged_kv* kv, const msd_block* blk,
+                                  const msd_ee_request* ee, void* k_rows, void* v_rows, int32_t window, int32_t sinks,
+                                  float* logits, int32_t* argmax, float* lse, void* ws, size_t ws_bytes,
+                                  hipStream_t stream) {
+  msd_status st = check_block(m, blk);
+  if (st != MSD_OK) return st;
+  PagedPass p{kv, {}, window, sinks, nullptr, 0};
+  st = check_cache(kv, &p.view);
+  if (st != MSD_OK) return st;
+  const msd_model_config& c = m->cfg;
+  if (kv->n_layers != c.n_layers || kv->n_kv_heads != c.n_kv_heads || kv->head_dim != c.head_dim)
+    return fail(MSD_ERR_SHAPE, "the paged cache has other layers, kv heads or head_dim than the model");
+  if (!k_rows || !v_rows || !aligned16(k_rows) || !aligned16(v_rows))
+    return fail(MSD_ERR_INVALID_ARG, "k_rows and v_rows must be 16-byte aligned device buffers");
+  if (window < 0 || sinks < 0) return fail(MSD_ERR_INVALID_ARG, "window and sinks must be >= 0");
+  if (p.view.capacity > c.max_positions) return fail(MSD_ERR_CAPACITY, "max_pages * page_size exceeds max_positions");
+  if (p.view.capacity < blk->n_slots) return fail(MSD_ERR_CAPACITY, "max_pages * page_size below n_slots");
+  if (blk->batch > kv->batch_cap) return fail(MSD_ERR_SHAPE, "batch exceeds the cache's batch_cap");
+  // the block's own rows as a cache of n_slots positions a sequence
+  msd_kv_cache rows{k_rows, v_rows, kv->len, kv->status, blk->batch, blk->n_slots};
+  Topo topo;
+  Layout L;
+  st = verify_prepare(m, &rows, blk, ee, argmax, &topo, &L);
+  if (st != MSD_OK) return st;
+  p.ws_bytes = msd_paged_attention_workspace_bytes(kv, blk->batch, blk->n_slots, c.n_heads);
+  if (!ws || !aligned16(ws) || ws_bytes < L.total + p.ws_bytes) return fail(MSD_ERR_WORKSPACE, "workspace too small");
+  char* w = static_cast<char*>(ws);
+  p.ws = w + L.total;
+  return verify_launch(m, &rows, blk, ee, logits, argmax, lse, w, topo, L, stream, &p);
+}
 
 msd_status msd_early_exit_topk(const msd_model* m, const float* hidden, int32_t M, int32_t kappa,
                                int32_t* ids, float* logp, void* ws, size_t ws_bytes,

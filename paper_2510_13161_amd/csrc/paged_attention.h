@@ -389,8 +389,9 @@ struct Core {
   // the rows' own keys; rotated ones enter as hi + lo, like the queries
   __device__ __forceinline__ void own_scores(floatx4 (&sc)[QPW][2], int first) {
     clear(sc);
+    const int parts = a.rope.table ? 2 : 1;
 #pragma unroll 1
-    for (int p = 0; p < QPARTS; ++p) {
+    for (int p = 0; p < parts; ++p) {
       stage_own(first, p);
       scores(sc, [&](int j, int kk) {
         return *reinterpret_cast<const bf16x8*>(vs + (16 * j + r16) * L::kVS + 8 * operand_group<FP8>(kk, g));
@@ -523,7 +524,15 @@ __device__ __forceinline__ void walk_apart(const Core<HD, FP8, QPW, ROT>& w, con
     for (int e = 0; e < HD / 64; ++e) {
       const int d = lane + 64 * e;
       if (partial) a.part_o[part * HD + d] = o[e];
-      else a.out[w.b * a.out_seq + slot * a.out_row + (w.kvh * G + gq) * a.out_head + d] = f2bf(o[e] * inv);
+    }
+    if (!partial) {  // 4 dims a lane, from the lanes that hold them
+#pragma unroll
+      for (int e = 0; e < HD / 64; ++e) {
+        float y[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) y[k] = __shfl(o[e], (4 * lane + k) & 63) * inv;
+        if (lane < 16) write_output(a, w.b, w.kvh * G + gq, slot, 64 * e + 4 * lane, y);
+      }
     }
   }
 }
@@ -608,6 +617,21 @@ __global__ __launch_bounds__(64 * kWaves, (Core<HD, FP8, QPW, ROT>::kTight) ? 4 
   for (int i = tid; i < QPW * 16 * (HD / 8); i += kThreads) {
     const int cg = i % (HD / 8), q = i / (HD / 8);
     const int t = q >> 4, qg = (qt0 + t) * 16 + (q & 15);
+    int kk, g;
+    operand_place<FP8>(cg, kk, g);
+    uint16_t* dst = q_sh + (((t * C::KSTEPS + kk) * C::QPARTS) * 64 + 16 * g + (q & 15)) * 8;
+    if (ROT && a.q_img) {  // already hi and lo, 8 dims a lane and k-step
+      bf16x8 hi = zero_bf16x8(), lo = hi;
+      if (qg < Qn) {
+        const uint16_t* src = a.q_img + (((size_t)b * a.kv.heads + kvh) * QT + qt0 + t) * (size_t)(C::KSTEPS * 1024) +
+                              (cg >> 2) * 1024 + (16 * (cg & 3) + (q & 15)) * 8;
+        hi = load16(src);
+        lo = load16(src + 512);
+      }
+      *reinterpret_cast<bf16x8*>(dst) = hi;
+      *reinterpret_cast<bf16x8*>(dst + 512) = lo;
+      continue;
+    }
     float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
     if (qg < Qn) {
       int gq, slot;
@@ -620,11 +644,8 @@ __global__ __launch_bounds__(64 * kWaves, (Core<HD, FP8, QPW, ROT>::kTight) ? 4 
 #pragma unroll
       for (int e = 0; e < 8; ++e) v[e] = -v[e];
     }
-    int kk, g;
-    operand_place<FP8>(cg, kk, g);
     bf16x8 hi, lo;
     split_vals(v, hi, lo);
-    uint16_t* dst = q_sh + (((t * C::KSTEPS + kk) * C::QPARTS) * 64 + 16 * g + (q & 15)) * 8;
     *reinterpret_cast<bf16x8*>(dst) = hi;
     if (ROT) *reinterpret_cast<bf16x8*>(dst + 512) = lo;
   }
@@ -679,8 +700,8 @@ __global__ __launch_bounds__(64 * kWaves, (Core<HD, FP8, QPW, ROT>::kTight) ? 4 
         query_of(a, qg, gq, slot);
         if (slot >= cnt) continue;
         const float inv = S != 0.0f ? 1.0f / S : 0.0f;
-        const u32x2 y = {pack_bf16x2(acc[0] * inv, acc[1] * inv), pack_bf16x2(acc[2] * inv, acc[3] * inv)};
-        *reinterpret_cast<u32x2*>(a.out + b * a.out_seq + slot * a.out_row + (kvh * G + gq) * a.out_head + 4 * c4) = y;
+        const float y[4] = {acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv};
+        write_output(a, b, kvh * G + gq, slot, 4 * c4, y);
       }
     }
   }
@@ -688,7 +709,7 @@ __global__ __launch_bounds__(64 * kWaves, (Core<HD, FP8, QPW, ROT>::kTight) ? 4 
 
 template <int HD, bool FP8, int QPW>
 void launch_core(const PagedAttnArgs& a, const Topo& topo, dim3 grid, hipStream_t s) {
-  if (a.rope.table) hipLaunchKernelGGL((paged_attn_kernel<HD, FP8, QPW, true>), grid, dim3(64 * kWaves), 0, s, a, topo);
+  if (a.rope.table || a.q_img) hipLaunchKernelGGL((paged_attn_kernel<HD, FP8, QPW, true>), grid, dim3(64 * kWaves), 0, s, a, topo);
   else hipLaunchKernelGGL((paged_attn_kernel<HD, FP8, QPW, false>), grid, dim3(64 * kWaves), 0, s, a, topo);
 }
 template <int HD, bool FP8>

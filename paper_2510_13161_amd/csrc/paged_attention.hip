@@ -58,11 +58,8 @@ __global__ __launch_bounds__(256) void paged_merge_kernel(PagedAttnArgs a) {
     }
   }
   const float inv = S != 0.0f ? 1.0f / S : 0.0f;
-  o0 *= inv;
-  o1 *= inv;
-  const u32x4 y = {pack_bf16x2(o0[0], o0[1]), pack_bf16x2(o0[2], o0[3]), pack_bf16x2(o1[0], o1[1]),
-                   pack_bf16x2(o1[2], o1[3])};
-  *reinterpret_cast<u32x4*>(a.out + b * a.out_seq + slot * a.out_row + (kvh * G + gq) * a.out_head + 8 * c8) = y;
+  const float y[8] = {o0[0] * inv, o0[1] * inv, o0[2] * inv, o0[3] * inv, o1[0] * inv, o1[1] * inv, o1[2] * inv, o1[3] * inv};
+  write_output(a, b, kvh * G + gq, slot, 8 * c8, y);
 }
 
 }  // namespace

@@ -98,5 +98,30 @@ __device__ __forceinline__ void query_of(const PagedAttnArgs& a, int qg, int& gq
   slot = qg - gq * a.n_slots;
 }
 
+// Where 4 (or 8) consecutive output dims of a query from dim d on go: rounded to
+// bf16, or as hi + lo words of the output projection's image.
+template <int N>
+__device__ __forceinline__ void write_output(const PagedAttnArgs& a, int b, int h, int slot, int d, const float (&o)[N]) {
+  uint32_t hi[N / 2], lo[N / 2];
+#pragma unroll
+  for (int i = 0; i < N / 2; ++i) {
+    hi[i] = pack_bf16x2(o[2 * i], o[2 * i + 1]);
+    lo[i] = pack_bf16x2(o[2 * i] - bf_lo(hi[i]), o[2 * i + 1] - bf_hi(hi[i]));
+  }
+  uint16_t* dst;
+  if (a.out_img) {
+    const int m = b * a.n_slots + slot, col = h * a.kv.head_dim + d;
+    dst = a.out_img + img_offset(col >> 5, m >> 4, a.MT, 16 * ((col >> 3) & 3) + (m & 15)) + (col & 7);
+  } else {
+    dst = a.out + b * a.out_seq + slot * a.out_row + h * a.out_head + d;
+  }
+#pragma unroll
+  for (int i = 0; i < N / 4; ++i) reinterpret_cast<u32x2*>(dst)[i] = u32x2{hi[2 * i], hi[2 * i + 1]};
+  if (a.out_img) {
+#pragma unroll
+    for (int i = 0; i < N / 4; ++i) reinterpret_cast<u32x2*>(dst + 512)[i] = u32x2{lo[2 * i], lo[2 * i + 1]};
+  }
+}
+
 }  // namespace
 }  // namespace msd

@@ -29,4 +29,11 @@ inline bool topo_from(const int32_t* parent, int n, Topo* t) {
   return true;
 }
 
+// Host checks of a paged cache, and its kernels' view of it.
+msd_status check_cache(const msd_paged_kv* kv, PagedView* v) noexcept;
+// Launches a (its cache, layer, block and queries filled in) with the partial
+// results in ws.
+msd_status run_paged_attention(const msd_paged_kv* kv, PagedAttnArgs a, const Topo& topo, void* ws, size_t ws_bytes,
+                               hipStream_t stream) noexcept;
+
 }  // namespace msd

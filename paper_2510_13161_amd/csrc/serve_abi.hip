@@ -15,28 +15,6 @@ bool stride_ok(int64_t s) { return s >= 0 && s % 8 == 0; }
 
 msd_status hip_fail(hipError_t e) { return e == hipSuccess ? MSD_OK : report(MSD_ERR_HIP, hipGetErrorString(e)); }
 
-msd_status check_cache(const msd_paged_kv* kv, PagedView* v) {
-  if (!kv) return report(MSD_ERR_INVALID_ARG, "null paged cache");
-  if (!kv->k || !kv->v || !kv->page_table || !kv->len || !kv->status)
-    return report(MSD_ERR_INVALID_ARG, "null paged cache field");
-  if (kv->format != MSD_KV_BF16 && kv->format != MSD_KV_FP8)
-    return report(MSD_ERR_UNSUPPORTED, "unknown paged cache format");
-  if (kv->format == MSD_KV_FP8 && (!kv->k_scale || !kv->v_scale))
-    return report(MSD_ERR_INVALID_ARG, "8-bit pages need k_scale and v_scale");
-  if (!aligned16(kv->k) || !aligned16(kv->v)) return report(MSD_ERR_INVALID_ARG, "k and v must be 16-byte aligned");
-  if (kv->head_dim != 64 && kv->head_dim != 128) return report(MSD_ERR_SHAPE, "head_dim must be 64 or 128");
-  int shift = 4;
-  while (shift <= 8 && (1 << shift) != kv->page_size) ++shift;
-  if (shift > 8) return report(MSD_ERR_SHAPE, "page_size must be 16, 32, 64, 128 or 256");
-  if (kv->n_layers < 1 || kv->n_pages < 1 || kv->n_kv_heads < 1 || kv->batch_cap < 1 || kv->max_pages < 1)
-    return report(MSD_ERR_SHAPE, "paged cache sizes must be >= 1");
-  const int64_t cap = (int64_t)kv->max_pages * kv->page_size;
-  if (cap > (int64_t)1 << 30) return report(MSD_ERR_CAPACITY, "max_pages * page_size above 2^30");
-  *v = PagedView{kv->k, kv->v, kv->k_scale, kv->v_scale, kv->page_table, kv->len, kv->status,
-                 kv->n_pages, kv->n_kv_heads, shift, kv->head_dim, kv->max_pages, cap};
-  return MSD_OK;
-}
-
 msd_status check_rope(const msd_rope* r, const PagedView& kv, RopeView* v) {
   *v = RopeView{nullptr, 0, 0};
   if (!r) return MSD_OK;
@@ -118,6 +96,52 @@ constexpr size_t kPagedPlanBytes = (kPagedPlanBatch + 4) * sizeof(int32_t);
 
 }  // namespace
 
+namespace msd {
+
+msd_status check_cache(const msd_paged_kv* kv, PagedView* v) noexcept {
+  if (!kv) return report(MSD_ERR_INVALID_ARG, "null paged cache");
+  if (!kv->k || !kv->v || !kv->page_table || !kv->len || !kv->status)
+    return report(MSD_ERR_INVALID_ARG, "null paged cache field");
+  if (kv->format != MSD_KV_BF16 && kv->format != MSD_KV_FP8)
+    return report(MSD_ERR_UNSUPPORTED, "unknown paged cache format");
+  if (kv->format == MSD_KV_FP8 && (!kv->k_scale || !kv->v_scale))
+    return report(MSD_ERR_INVALID_ARG, "8-bit pages need k_scale and v_scale");
+  if (!aligned16(kv->k) || !aligned16(kv->v)) return report(MSD_ERR_INVALID_ARG, "k and v must be 16-byte aligned");
+  if (kv->head_dim != 64 && kv->head_dim != 128) return report(MSD_ERR_SHAPE, "head_dim must be 64 or 128");
+  int shift = 4;
+  while (shift <= 8 && (1 << shift) != kv->page_size) ++shift;
+  if (shift > 8) return report(MSD_ERR_SHAPE, "page_size must be 16, 32, 64, 128 or 256");
+  if (kv->n_layers < 1 || kv->n_pages < 1 || kv->n_kv_heads < 1 || kv->batch_cap < 1 || kv->max_pages < 1)
+    return report(MSD_ERR_SHAPE, "paged cache sizes must be >= 1");
+  const int64_t cap = (int64_t)kv->max_pages * kv->page_size;
+  if (cap > (int64_t)1 << 30) return report(MSD_ERR_CAPACITY, "max_pages * page_size above 2^30");
+  *v = PagedView{kv->k, kv->v, kv->k_scale, kv->v_scale, kv->page_table, kv->len, kv->status,
+                 kv->n_pages, kv->n_kv_heads, shift, kv->head_dim, kv->max_pages, cap};
+  return MSD_OK;
+}
+
+msd_status run_paged_attention(const msd_paged_kv* kv, PagedAttnArgs a, const Topo& topo, void* ws, size_t ws_bytes,
+                               hipStream_t stream) noexcept {
+  // blocks that a sequence can have: of its whole capacity, or of the sinks and the window
+  int64_t blocks = (a.kv.capacity + 31) / 32;
+  if (a.window > 0)
+    blocks = std::min(blocks, ((int64_t)a.sinks + 31) / 32 + ((int64_t)a.window + a.n_slots + 30) / 32 + 1);
+  if (a.k_new) blocks += (a.n_slots + 31) / 32;
+  const PagedShape sh = paged_shape(kv, a.batch, a.n_slots, a.n_heads, blocks);
+  a.q_per_wg = sh.q_per_wg;
+  a.groups = sh.groups;
+  a.wgs = sh.wgs;
+  const size_t rows = (size_t)sh.wgs * kv->n_kv_heads * sh.groups * sh.q_per_wg * 16;
+  a.plan = static_cast<int32_t*>(ws);
+  a.part_o = reinterpret_cast<float*>(static_cast<char*>(ws) + kPagedPlanBytes);
+  a.part_ml = a.part_o + rows * kv->head_dim;
+  if (kPagedPlanBytes + paged_partials(sh, kv->n_kv_heads, kv->head_dim) > ws_bytes)
+    return report(MSD_ERR_WORKSPACE, "workspace too small");
+  return hip_fail(launch_paged_attention(kv->format == MSD_KV_FP8, a, topo, stream));
+}
+
+}  // namespace msd
+
 extern "C" {
 
 msd_status msd_paged_append(const msd_paged_kv* kv, const msd_kv_rows* rows, const msd_rope* rope,
@@ -188,21 +212,6 @@ msd_status msd_paged_attention(const msd_paged_kv* kv, int32_t layer, const msd_
   if (!ws || !aligned16(ws) ||
       ws_bytes < msd_paged_attention_workspace_bytes(kv, at->batch, at->n_slots, at->n_heads))
     return report(MSD_ERR_WORKSPACE, "workspace NULL, unaligned or too small");
-  // blocks that a sequence can have: of its whole capacity, or of the sinks and the window
-  int64_t blocks = (a.kv.capacity + 31) / 32;
-  if (at->window > 0)
-    blocks = std::min(blocks, ((int64_t)at->sinks + 31) / 32 + ((int64_t)at->window + at->n_slots + 30) / 32 + 1);
-  if (at->k_new) blocks += (at->n_slots + 31) / 32;
-  const PagedShape sh = paged_shape(kv, at->batch, at->n_slots, at->n_heads, blocks);
-  a.q_per_wg = sh.q_per_wg;
-  a.groups = sh.groups;
-  a.wgs = sh.wgs;
-  const size_t rows = (size_t)sh.wgs * kv->n_kv_heads * sh.groups * sh.q_per_wg * 16;
-  a.plan = static_cast<int32_t*>(ws);
-  a.part_o = reinterpret_cast<float*>(static_cast<char*>(ws) + kPagedPlanBytes);
-  a.part_ml = a.part_o + rows * kv->head_dim;
-  if (kPagedPlanBytes + paged_partials(sh, kv->n_kv_heads, kv->head_dim) > ws_bytes)
-    return report(MSD_ERR_WORKSPACE, "workspace too small");
   a.layer = layer;
   a.q = static_cast<const uint16_t*>(at->q);
   a.q_seq = at->q_seq;
@@ -224,7 +233,7 @@ msd_status msd_paged_attention(const msd_paged_kv* kv, int32_t layer, const msd_
   a.n_heads = at->n_heads;
   a.window = at->window;
   a.sinks = at->sinks;
-  return hip_fail(launch_paged_attention(kv->format == MSD_KV_FP8, a, topo, stream));
+  return run_paged_attention(kv, a, topo, ws, ws_bytes, stream);
 }
 
 size_t msd_sample_workspace_bytes(int32_t rows, int32_t vocab) {

@@ -34,7 +34,8 @@ EXPORTED = ["msd_last_error", "msd_model_create", "msd_model_destroy", "msd_work
             "msd_verify_block", "msd_early_exit_topk", "msd_accept", "msd_kv_commit",
             "msd_reuse_select", "msd_set_profile", "msd_verify_block_static",
             "msd_paged_append", "msd_paged_commit", "msd_paged_attention",
-            "msd_paged_attention_workspace_bytes", "msd_sample", "msd_sample_workspace_bytes"]
+            "msd_paged_attention_workspace_bytes", "msd_sample", "msd_sample_workspace_bytes",
+            "msd_verify_block_paged", "msd_verify_paged_workspace_bytes"]
 MSD_STATIC_SCRATCH_BYTES = 64 << 20
 MSD_ACCEPT_WS_PER_ROW = 1024  # bytes a row of the acceptance workspace (msd.h)
 MSD_K_QKV, MSD_K_ATTN, MSD_K_OPROJ, MSD_K_FFN_UP, MSD_K_FFN_DOWN = 0, 1, 2, 3, 4
@@ -160,13 +161,16 @@ def lib() -> ctypes.CDLL:
         L.msd_paged_attention.argtypes = [P, i32, P, P, ctypes.c_size_t, P]
         L.msd_paged_attention_workspace_bytes.argtypes = [P, i32, i32, i32]
         L.msd_paged_attention_workspace_bytes.restype = ctypes.c_size_t
+        L.msd_verify_block_paged.argtypes = [P, P, P, P, P, P, i32, i32, P, P, P, P, ctypes.c_size_t, P]
+        L.msd_verify_paged_workspace_bytes.argtypes = [P, P, i32, i32, i32]
+        L.msd_verify_paged_workspace_bytes.restype = ctypes.c_size_t
         L.msd_sample.argtypes = [P, ctypes.c_int64, i32, i32, P, P, P, P, P, P, ctypes.c_size_t, P]
         L.msd_sample_workspace_bytes.argtypes = [i32, i32]
         L.msd_sample_workspace_bytes.restype = ctypes.c_size_t
         for f in ("msd_model_create", "msd_verify_block", "msd_verify_block_static",
                   "msd_early_exit_topk", "msd_accept",
                   "msd_kv_commit", "msd_reuse_select", "msd_set_profile", "msd_paged_append",
-                  "msd_paged_commit", "msd_paged_attention", "msd_sample"):
+                  "msd_paged_commit", "msd_paged_attention", "msd_sample", "msd_verify_block_paged"):
             getattr(L, f).restype = ctypes.c_int
         _lib = L
     return _lib
@@ -336,6 +340,23 @@ def paged_attention(kv: PagedKV, layer: int, attn: PagedAttn, ws: torch.Tensor, 
     _fits(kv, attn)
     _check(lib().msd_paged_attention(ctypes.byref(kv), layer, ctypes.byref(attn), _ptr(ws),
                                      _nbytes(ws), _stream(stream)))
+
+
+def verify_paged_workspace_bytes(handle, kv: PagedKV, batch: int, n_slots: int, kappa: int) -> int:
+    return int(lib().msd_verify_paged_workspace_bytes(handle, ctypes.byref(kv), batch, n_slots, kappa))
+
+
+def verify_block_paged(handle, kv: PagedKV, block: Block, ee: Optional[EERequest], k_rows: torch.Tensor,
+                       v_rows: torch.Tensor, logits, argmax, lse, ws: torch.Tensor, window: int = 0, sinks: int = 0,
+                       stream=None) -> None:
+    """k_rows, v_rows: bf16 [n_layers][batch][kv_heads][n_slots][head_dim], written; block_rows() commits them."""
+    shape = (kv.n_layers, block.batch, kv.n_kv_heads, block.n_slots, kv.head_dim)
+    _typed(k_rows, torch.bfloat16, shape, "k_rows")
+    _typed(v_rows, torch.bfloat16, shape, "v_rows")
+    _check(lib().msd_verify_block_paged(handle, ctypes.byref(kv), ctypes.byref(block),
+                                        ctypes.byref(ee) if ee is not None else None, _ptr(k_rows), _ptr(v_rows),
+                                        int(window), int(sinks), _ptr(logits), _ptr(argmax), _ptr(lse), _ptr(ws),
+                                        _nbytes(ws), _stream(stream)))
 
 
 def sample_workspace_bytes(rows: int, vocab: int) -> int:
@@ -515,6 +536,11 @@ def kv_rows(k: torch.Tensor, v: torch.Tensor, layer: int = 0, count: Optional[to
     r._keep = (k, v, count)
     r._heads, r._device = tuple(k.shape[3:]), k.device.index
     return r
+
+
+def block_rows(k_rows: torch.Tensor, v_rows: torch.Tensor) -> KVRows:
+    """The rows that verify_block_paged wrote, as paged_commit takes them."""
+    return kv_rows(k_rows.transpose(2, 3), v_rows.transpose(2, 3))
 
 
 def paged_attn(q: torch.Tensor, out: torch.Tensor, k_new: Optional[torch.Tensor] = None,
