@@ -7,22 +7,21 @@
 // histograms may be filled with atomics and a run repeats bit for bit (2^20
 // tokens of mass one fill 2^63).
 //
-//  1 top    a workgroup a chunk of 8192 logits: its largest.
-//  2 tally  the chunk again (held in registers, 16 a thread): its mass where the row
-//           needs the mass of all tokens (unfiltered, or top-p without top-k); for
-//           filtered rows a histogram over half octaves of 2^t down to
-//           2^-64, of counts and, for top-p without top-k, masses; and the keys of
-//           the chunk's highest half octaves, in their order, as many as fit 512.
-//  3 draw   a workgroup a row: the histograms added up give the half octave that
-//           top-k (else top-p, min-p) cuts. Where the chunks' lists reach
-//           down to it, its keys and those above come into LDS; a cut is found by a
-//           histogram over 1024 parts of its half octave, the few keys of one
-//           part then ranked by counting. Else (flat laws, whose kept sets are a
-//           large part of the vocabulary) digit by digit over the row. The draw:
-//           masses of 512-id segments, the segment, the id. Unfiltered rows
-//           take the chunk from the chunks' masses.
-// 144 rows of 152K logits: 87.6 MB, read twice (the second time mostly from the
-// memory-side cache).
+//  1 tally  a workgroup a chunk of 8192 logits, held in registers: the largest; where
+//           the row needs the mass of all tokens (unfiltered, or top-p without
+//           top-k) the chunk's, against its own largest; for filtered rows the
+//           chunk's highest tokens: a histogram of counts over half octaves below its
+//           largest says how many half octaves fit the chunk's share of
+//           4096 keys, and those are listed.
+//  2 draw   a workgroup a row, the lists in its registers. A cut is found by a histogram of
+//           counts and masses over half octaves below the row's largest, then over
+//           1024 parts of one half octave, then by ranking the few keys of one
+//           part. It stands if every chunk has listed all it has above it; else
+//           (flat laws, whose kept sets are a large part of the vocabulary) it is
+//           searched digit by digit over the row. The draw: masses of 512-id
+//           segments, the segment, the id. Unfiltered rows take the chunk from the
+//           chunks' masses.
+// The logits are read once: 144 rows of 152K are 87.6 MB.
 #include <algorithm>
 
 #include "sample.h"
@@ -31,53 +30,39 @@ namespace msd {
 namespace {
 
 constexpr int kTally = 512;       // threads of a chunk
-// Logits a thread of a chunk holds: 16 (chunks of 8192), or 4 where all chunks of
-// that size are fewer than the compute units (one row of 152K: 19 of 8192 or 75 of 2048).
-constexpr int kFew = 4, kMany = 16;
+// Logits a thread of a chunk holds: 16 (chunks of 8192), or 8 where all chunks of
+// that size are fewer than the compute units (one row of 152K: 19 of 8192 or 38 of 4096).
+constexpr int kFew = 8, kMany = 16;
 constexpr int kBins = 128;        // half octaves; the last takes all below 2^-63.5
-constexpr int kList = 512;        // keys of a chunk's list
 constexpr int kDraw = 1024;       // threads of the draw
-constexpr int kCands = 8192;      // keys that the draw holds
+constexpr int kCands = 4096;      // keys that the draw holds in registers: all chunks' lists
 constexpr int kSeg = 512;         // ids of a segment
 constexpr int kSegs = (1 << 20) / kSeg;
 constexpr int kMaxChunks = 256;
 constexpr int kDigit = 2048;      // digit values of the search over a row
 
 struct Chunk {
-  int32_t list_bin;  // the list holds all its tokens of bins <= list_bin, in order of bins
-  int32_t unused;
-  uint64_t mass;     // of all its tokens
-  uint64_t tokens;   // above -inf
+  uint32_t top;      // ordered bits of its largest logit, kDead: no token
+  int32_t list_bin;  // its list holds all its tokens of half octaves <= list_bin below its largest
+  uint32_t n_list;
+  uint32_t tokens;   // above -inf
+  uint64_t mass;     // of all its tokens, 2^-43 of its largest's
 };
 
-// Workspace of a row: [chunks] top keys, Chunk records, counts through each bin
-// [kBins], masses of the bins [kBins], lists [kList].
+// Workspace of a row: lists [chunks][kCands / chunks], Chunk records.
 struct Work {
-  uint32_t* top;
-  Chunk* head;
-  uint32_t* cnt;
-  uint64_t* mass;
   uint64_t* list;
+  Chunk* head;
 };
 // the larger chunks also where the smaller ones would be more than kMaxChunks
-inline int each_of(int rows, int vocab) {
-  const int many = (vocab + kTally * kMany - 1) / (kTally * kMany), few = (vocab + kTally * kFew - 1) / (kTally * kFew);
-  return (int64_t)rows * many < 256 && few <= kMaxChunks ? kFew : kMany;
-}
 inline int chunks_of(int each, int vocab) { return (vocab + kTally * each - 1) / (kTally * each); }
-__host__ __device__ inline size_t row_bytes(int C) {
-  const size_t b = (size_t)C * (kList * 8 + kBins * 12 + sizeof(Chunk) + 4);
-  return (b + 15) / 16 * 16;
+inline int each_of(int rows, int vocab) {
+  return (int64_t)rows * chunks_of(kMany, vocab) < 256 && chunks_of(kFew, vocab) <= kMaxChunks ? kFew : kMany;
 }
+__host__ __device__ inline size_t row_bytes(int C) { return (kCands * 8 + (size_t)C * sizeof(Chunk) + 15) / 16 * 16; }
 __device__ __forceinline__ Work work_of(const SampleArgs& a, int row, int C) {
   char* p = static_cast<char*>(a.ws) + row_bytes(C) * row;
-  Work w;
-  w.list = reinterpret_cast<uint64_t*>(p);
-  w.mass = w.list + (size_t)C * kList;
-  w.head = reinterpret_cast<Chunk*>(w.mass + (size_t)C * kBins);
-  w.cnt = reinterpret_cast<uint32_t*>(w.head + C);
-  w.top = w.cnt + (size_t)C * kBins;
-  return w;
+  return Work{reinterpret_cast<uint64_t*>(p), reinterpret_cast<Chunk*>(p + kCands * 8)};
 }
 
 // Half octave of a logit, in fp32: any function does that never rises with z and is
@@ -86,8 +71,8 @@ __device__ __forceinline__ Work work_of(const SampleArgs& a, int row, int C) {
 __device__ __forceinline__ float depth_of(float z, float ref, float c4) { return (0.5f * ref - 0.5f * z) * c4; }
 __device__ __forceinline__ int bin_of(float x) { return (int)fminf(x, (float)(kBins - 1)); }
 __device__ __forceinline__ float c4_of(const Request& q) { return (float)fmin(4.0 * q.c, 3e38); }
-// whether the row needs the mass of tokens that no list may hold
-__device__ __forceinline__ bool mass_by_bin(const Request& q, int V) { return q.p < 1.0 && q.k >= (uint32_t)V; }
+// whether top-p is a share of the mass of tokens that no list may hold
+__device__ __forceinline__ bool share_of_all(const Request& q, int V) { return q.p < 1.0 && q.k >= (uint32_t)V; }
 
 __device__ __forceinline__ uint32_t wave_max_u32(uint32_t v) {
 #pragma unroll
@@ -132,35 +117,13 @@ __device__ __forceinline__ void load4(const float* z, int i, int V, float* v) {
   }
 }
 
-template <int EACH>
-__global__ __launch_bounds__(kTally) void top_kernel(SampleArgs a) {
-  __shared__ uint32_t red[kTally / 64];
-  const int c = blockIdx.x, row = blockIdx.y, tid = threadIdx.x;
-  const float* z = a.logits + (int64_t)row * a.row_stride;
-  float v[EACH];
-#pragma unroll
-  for (int j = 0; j < EACH; j += 4) load4(z, c * (kTally * EACH) + j * kTally + 4 * tid, a.vocab, v + j);
-  float top = v[0];
-#pragma unroll
-  for (int j = 1; j < EACH; ++j) top = fmaxf(top, v[j]);
-  const uint32_t m = wave_max_u32(ordered_bits(top));
-  if ((tid & 63) == 0) red[tid >> 6] = m;
-  __syncthreads();
-  if (tid == 0) {
-    uint32_t t = red[0];
-    for (int w = 1; w < kTally / 64; ++w) t = max(t, red[w]);
-    work_of(a, row, gridDim.x).top[c] = t;
-  }
-}
-
 constexpr int kCopies = 4;  // of the histogram, by lane: tokens of one bin meet less often
 template <int EACH>
 __global__ __launch_bounds__(kTally) void tally_kernel(SampleArgs a) {
   __shared__ uint32_t cnt[kBins * kCopies];
-  __shared__ unsigned long long mass[kBins * kCopies];
   __shared__ uint32_t cursor[kBins];
   __shared__ uint64_t red[kTally / 64];
-  __shared__ uint32_t red_n[kTally / 64];
+  __shared__ uint32_t red_n[kTally / 64], red_top[kTally / 64];
   __shared__ uint32_t last_bin;
   __shared__ int list_bin;
   const int C = gridDim.x, c = blockIdx.x, row = blockIdx.y, tid = threadIdx.x;
@@ -170,17 +133,24 @@ __global__ __launch_bounds__(kTally) void tally_kernel(SampleArgs a) {
   float v[EACH];
 #pragma unroll
   for (int j = 0; j < EACH; j += 4) load4(z, first + j * kTally, a.vocab, v + j);
-  uint32_t top = 0;
-  for (int i = tid & 63; i < C; i += 64) top = max(top, w.top[i]);
   const Request q = request_of(a, row);
-  top = wave_max_u32(top);
-  if (top <= kDead) return;  // no token
+  for (int i = tid; i < kBins * kCopies; i += kTally) cnt[i] = 0;
+  if (tid == 0) last_bin = 0;
+  float most = v[0];
+#pragma unroll
+  for (int j = 1; j < EACH; ++j) most = fmaxf(most, v[j]);
+  uint32_t top = wave_max_u32(ordered_bits(most));
+  if ((tid & 63) == 0) red_top[tid >> 6] = top;
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < kTally / 64; ++i) top = max(top, red_top[i]);
+  if (top <= kDead) {
+    if (tid == 0) w.head[c] = Chunk{kDead, kBins - 1, 0, 0, 0};
+    return;
+  }
   const float ref = from_ordered_bits(top);
   const float c4 = c4_of(q);
-  const bool filtered = q.filtered(), by_bin = mass_by_bin(q, a.vocab);
-  for (int i = tid; i < kBins * kCopies; i += kTally) cnt[i] = 0, mass[i] = 0;
-  if (tid == 0) last_bin = 0;
-  __syncthreads();
+  const bool filtered = q.filtered(), need_mass = !filtered || share_of_all(q, a.vocab);
   uint64_t sum = 0;
   uint32_t tokens = 0;
   uint32_t low = 0;  // tokens of the last bin, which most tokens of cold laws share
@@ -189,19 +159,18 @@ __global__ __launch_bounds__(kTally) void tally_kernel(SampleArgs a) {
   for (int j = 0; j < EACH; ++j) {
     if (v[j] == -INFINITY) continue;
     ++tokens;
-    uint64_t m = 0;
-    if (!filtered || by_bin) sum += m = mass_of(exponent_of(v[j], ref, q.c));
+    if (need_mass) sum += mass_of(exponent_of(v[j], ref, q.c));
     if (!filtered) continue;
     const int b = bin_of(depth_of(v[j], ref, c4));
     if (b == kBins - 1) ++low;
     else atomicAdd(&cnt[b * kCopies + copy], 1u);
-    if (m) atomicAdd(&mass[b * kCopies + copy], (unsigned long long)m);
   }
   sum = wave_sum_u64(sum);
   tokens = (uint32_t)wave_sum_u64(tokens);
   if (low) atomicAdd(&last_bin, low);
   if ((tid & 63) == 0) red[tid >> 6] = sum, red_n[tid >> 6] = tokens;
   __syncthreads();
+  const uint32_t room = (uint32_t)(kCands / C);
   if (tid < 64) {
     // counts through each bin; the deepest bin down to which they fit the list
     uint32_t c0 = 0, c1 = 0;
@@ -209,49 +178,46 @@ __global__ __launch_bounds__(kTally) void tally_kernel(SampleArgs a) {
     for (int k = 0; k < kCopies; ++k) c0 += cnt[2 * tid * kCopies + k], c1 += cnt[(2 * tid + 1) * kCopies + k];
     if (tid == 63) c1 = last_bin;
     const uint32_t x = (uint32_t)wave_scan_u64(c0 + c1);
-    const int f = (int)__popcll(__ballot(x - c1 <= kList)) + (int)__popcll(__ballot(x <= kList));
+    const unsigned long long f0 = __ballot(x - c1 <= room), f1 = __ballot(x <= room);
+    const int f = (int)__popcll(f0) + (int)__popcll(f1);
     cursor[2 * tid] = x - c1 - c0;
     cursor[2 * tid + 1] = x - c1;
-    if (filtered) {
-      w.cnt[(size_t)c * kBins + 2 * tid] = x - c1;
-      w.cnt[(size_t)c * kBins + 2 * tid + 1] = x;
-    }
+    // tokens through the last bin that fits, bin f - 1 (lane (f - 1) / 2's second or first)
+    const uint32_t through = f & 1 ? x - c1 : x;
+    const uint32_t n_list = f ? (uint32_t)__builtin_amdgcn_readlane((int)through, (f - 1) >> 1) : 0u;
     if (tid == 0) {
       list_bin = f - 1;
       uint64_t s = red[0], n = red_n[0];
       for (int i = 1; i < kTally / 64; ++i) s += red[i], n += red_n[i];
-      w.head[c] = Chunk{f - 1, 0, s, n};
+      w.head[c] = Chunk{top, f - 1, filtered ? n_list : 0u, (uint32_t)n, s};
     }
   }
   if (!filtered) return;
-  if (by_bin && tid >= 64 && tid < 64 + kBins) {
-    uint64_t m = 0;
-#pragma unroll
-    for (int k = 0; k < kCopies; ++k) m += mass[(tid - 64) * kCopies + k];
-    w.mass[(size_t)c * kBins + tid - 64] = m;
-  }
   __syncthreads();
   const int lb = list_bin;
 #pragma unroll
   for (int j = 0; j < EACH; ++j) {
     const int b = v[j] == -INFINITY ? kBins : bin_of(depth_of(v[j], ref, c4));
     if (b <= lb)
-      w.list[(size_t)c * kList + atomicAdd(&cursor[b], 1u)] = rank_key(v[j], first + kTally * (j & ~3) + (j & 3));
+      w.list[(size_t)c * room + atomicAdd(&cursor[b], 1u)] = rank_key(v[j], first + kTally * (j & ~3) + (j & 3));
   }
 }
 
+constexpr int kHeld = kCands / kDraw;  // keys of a thread
+
 struct Shared {
-  uint64_t cand[kCands];       // keys; in the search over a row: digit masses
-  uint64_t seg[kSegs];         // segment masses; before, the search among the keys
+  uint64_t seg[kSegs];         // segment masses; in the searches, their own tables
+  uint64_t more[kDraw];        // their other tables
   uint64_t red[2][kDraw / 64];
-  uint64_t mass[kBins];        // tokens of the bins above, then of the bin
-  uint32_t cnt[kBins];
+  uint64_t mass[kBins];        // of the keys through each bin
+  uint32_t cnt[kBins];         // keys through each bin
   uint64_t above_mass, above, key;
+  uint32_t top[kDraw / 64];
   uint32_t n, m, pick;
-  int min_list;
-  uint32_t from[kMaxChunks + 1];  // candidates of the chunks before
+  uint32_t n_list[kMaxChunks];
 };
-static_assert(kCands * 8 >= kDigit * 12, "digit histograms fit the key list");
+static_assert(kBins * kCopies <= kDraw, "a thread for each bin of the copies");
+static_assert(kSegs >= kDigit && 2 * kDraw >= kDigit, "masses and counts of the digits");
 
 // Inclusive scan over the block, and the block's sum. One barrier: wave sums go to
 // one of two places in turn, so that a wave that is a scan ahead overwrites none.
@@ -298,8 +264,8 @@ struct Row {
 // cut in id order.
 template <bool BY_MASS>
 __device__ uint64_t search_row(Shared& sh, Scan& scan, const Row& r, uint64_t n, double want, uint64_t floor) {
-  uint64_t* mass = sh.cand;
-  uint32_t* cnt = reinterpret_cast<uint32_t*>(mass + kDigit);
+  uint64_t* mass = sh.seg;
+  uint32_t* cnt = reinterpret_cast<uint32_t*>(sh.more);
   const int tid = threadIdx.x;
   uint32_t prefix = 0;
   uint64_t above = 0, above_mass = 0;
@@ -378,42 +344,43 @@ __device__ uint64_t search_row(Shared& sh, Scan& scan, const Row& r, uint64_t n,
   return sh.key;
 }
 
-// The same among the candidate keys >= floor of bin `bin`, which has `size`;
-// `above` tokens and `above_mass` lie in the bins before. More than kRanked keys
-// are first narrowed to the part of the bin (1024, a thread each) in which the prefix
-// ends; the keys that remain are ranked by counting. False: more of those than
-// threads (equal logits).
+// The same among the listed keys >= floor (a thread holds kHeld of them, 0: none) of
+// bin `bin`, which has `size`; `above` tokens and `above_mass` lie in the bins before.
+// More than kRanked keys are first narrowed to the part of the bin (1024, a thread
+// each) in which the prefix ends; the keys that remain are ranked by counting.
+// False: more of those than threads (equal logits).
 constexpr uint32_t kRanked = 256;
 template <bool BY_MASS>
-__device__ bool search_bin(Shared& sh, Scan& scan, const Row& r, uint32_t N, int bin, uint32_t size, uint64_t n,
-                           double want, uint64_t above, uint64_t above_mass, uint64_t floor, uint64_t* key_out, uint64_t* kept_mass) {
+__device__ __forceinline__ bool search_bin(Shared& sh, Scan& scan, const Row& r, const uint64_t (&held)[kHeld], int bin,
+                                           uint32_t size, uint64_t n, double want, uint64_t above, uint64_t above_mass,
+                                           uint64_t floor, uint64_t* key_out) {
   const int tid = threadIdx.x;
-  uint64_t* mass = sh.seg;                                       // [kDraw]
-  uint32_t* cnt = reinterpret_cast<uint32_t*>(sh.seg + kDraw);   // [kDraw]
+  uint64_t* mass = sh.more;                             // [kDraw]
+  uint32_t* cnt = reinterpret_cast<uint32_t*>(sh.seg);  // [kDraw]
   auto part_of = [&](uint64_t k) {  // -1: not of the bin
+    if (k < floor || k == 0) return -1;
     const float x = r.depth(k);
     return bin_of(x) != bin ? -1 : (int)fminf((x - (float)bin) * kDraw, (float)(kDraw - 1));
   };
   auto inside = [&](uint64_t cb, uint64_t mb) { return BY_MASS ? (cb == 0 || (double)mb < want) : cb < n; };
   int part = -2;  // any
   __syncthreads();
-  mass[tid] = 0;
-  cnt[tid] = 0;
   if (tid == 0) sh.m = 0, sh.n = 0;
-  __syncthreads();
   if (size > kRanked) {
-    for (uint32_t i = tid; i < N; i += kDraw) {
-      const uint64_t k = sh.cand[i];
-      if (k < floor) continue;
-      const int p = part_of(k);
+    cnt[tid] = 0;
+    if (BY_MASS) mass[tid] = 0;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kHeld; ++i) {
+      const int p = part_of(held[i]);
       if (p < 0) continue;
       atomicAdd(&cnt[p], 1u);
-      atomicAdd((unsigned long long*)&mass[p], (unsigned long long)r.mass(k));
+      if (BY_MASS) atomicAdd((unsigned long long*)&mass[p], (unsigned long long)r.mass(held[i]));
     }
     __syncthreads();
-    const uint64_t c0 = cnt[tid], m0 = mass[tid];
+    const uint64_t c0 = cnt[tid], m0 = BY_MASS ? mass[tid] : 0;
     const uint64_t cb = above + scan(c0) - c0;
-    const uint64_t mb = above_mass + scan(m0) - m0;
+    const uint64_t mb = BY_MASS ? above_mass + scan(m0) - m0 : 0;
     const bool in = c0 && inside(cb, mb);  // a prefix of the parts
     if (in) atomicMax(&sh.m, (uint32_t)tid);
     __syncthreads();
@@ -423,12 +390,14 @@ __device__ bool search_bin(Shared& sh, Scan& scan, const Row& r, uint32_t N, int
     above = sh.above;
     above_mass = sh.above_mass;
     if (sh.pick > kDraw) return false;
+  } else {
+    __syncthreads();
   }
   uint64_t* mine = sh.seg;
-  for (uint32_t i = tid; i < N; i += kDraw) {
-    const uint64_t k = sh.cand[i];
-    const int p = part_of(k);
-    if (k >= floor && p >= 0 && (part < 0 || p == part)) mine[atomicAdd(&sh.n, 1u)] = k;
+#pragma unroll
+  for (int i = 0; i < kHeld; ++i) {
+    const int p = part_of(held[i]);
+    if (p >= 0 && (part < 0 || p == part)) mine[atomicAdd(&sh.n, 1u)] = held[i];
   }
   __syncthreads();
   const uint32_t m = sh.n;
@@ -436,8 +405,15 @@ __device__ bool search_bin(Shared& sh, Scan& scan, const Row& r, uint32_t N, int
   uint32_t rank = 0;
 #pragma unroll 8
   for (uint32_t i = 0; i < m; ++i) rank += mine[i] > key;
-  __syncthreads();
-  uint64_t* by_rank = sh.seg;               // masses
+  if (!BY_MASS) {  // the token of rank n - 1, or the last
+    const uint64_t last = n - above < m ? n - above : m;
+    if (tid < (int)m && rank == last - 1) sh.key = key;
+    __syncthreads();
+    *key_out = sh.key;
+    __syncthreads();
+    return true;
+  }
+  uint64_t* by_rank = sh.more;              // masses
   uint64_t* key_by_rank = sh.seg + kDraw;
   if (tid < (int)m) {
     by_rank[rank] = r.mass(key);
@@ -447,13 +423,10 @@ __device__ bool search_bin(Shared& sh, Scan& scan, const Row& r, uint32_t N, int
   const uint64_t w = tid < (int)m ? by_rank[tid] : 0;
   const uint64_t x = above_mass + scan(w);  // mass through rank tid
   // the ranks inside are a prefix: the last of them
-  if (tid < (int)m && inside(above + tid, x - w) && (tid + 1 == (int)m || !inside(above + tid + 1, x))) {
+  if (tid < (int)m && inside(above + tid, x - w) && (tid + 1 == (int)m || !inside(above + tid + 1, x)))
     sh.key = key_by_rank[tid];
-    sh.above_mass = x;
-  }
   __syncthreads();
   *key_out = sh.key;
-  *kept_mass = sh.above_mass;
   __syncthreads();
   return true;
 }
@@ -468,9 +441,15 @@ __global__ __launch_bounds__(kDraw) void draw_kernel(SampleArgs a, int C, int ch
   r.z = a.logits + (int64_t)row * a.row_stride;
   r.V = a.vocab;
   r.q = request_of(a, row);
-  uint32_t top = 0;
-  for (int i = lane; i < C; i += 64) top = max(top, w.top[i]);
-  r.top = wave_max_u32(top);
+  const Chunk head = tid < C ? w.head[tid] : Chunk{kDead, kBins - 1, 0, 0, 0};
+  {
+    const uint32_t top = wave_max_u32(head.top);
+    if (lane == 0) sh.top[wave] = top;
+    __syncthreads();
+    r.top = sh.top[0];
+#pragma unroll
+    for (int i = 1; i < kDraw / 64; ++i) r.top = max(r.top, sh.top[i]);
+  }
   if (r.top <= kDead) {
     if (tid == 0) {
       a.tok[row] = -1;
@@ -486,43 +465,70 @@ __global__ __launch_bounds__(kDraw) void draw_kernel(SampleArgs a, int C, int ch
   uint32_t n_kept = 0;
   const int n_seg = (r.V + kSeg - 1) / kSeg;
   int first_seg = 0, last_seg = n_seg;  // segments whose masses are in sh.seg
-  uint64_t total = 0, before = 0;       // all kept mass; that of the segments before first_seg
+  uint64_t total = 0;                   // all kept mass
+  double part = r.q.u;                  // share of the segments' mass at which the draw lies
+  const float ref = r.ref;
   bool from_list = false;
-  uint32_t N = 0;
 
+  // the chunks' masses against the row's largest
+  const double down = head.top > kDead ? exponent_of(from_ordered_bits(head.top), r.ref, r.q.c) : 0.0;
+  const uint64_t chunk_mass = head.mass ? (uint64_t)((double)head.mass * exp2_64(down, 0) + 0.5) : 0;
+  const uint32_t valid = (uint32_t)(scan(head.tokens), scan.sum);
+
+  uint64_t held[kHeld];  // listed keys of this thread, 0: none
   if (filtered) {
-    const bool by_bin = mass_by_bin(r.q, r.V);
-    if (tid < kBins) sh.cnt[tid] = 0, sh.mass[tid] = 0;
-    if (tid == 0) sh.min_list = kBins;
+    const bool of_all = share_of_all(r.q, r.V), by_k = r.q.k < valid;
+    bool by_p = r.q.p < 1.0;
+    uint64_t all = 0;  // mass that top-p is a share of
+    if (of_all) scan(chunk_mass), all = scan.sum;
+    scan(head.n_list);
+    const uint32_t N = (uint32_t)scan.sum;
+    if (tid < C) sh.n_list[tid] = head.n_list;
     __syncthreads();
-    {
-      uint32_t n = 0;
-      uint64_t m = 0;
-      const int b = tid % kBins;
-#pragma unroll 8
-      for (int c = tid / kBins; c < C; c += kDraw / kBins) n += w.cnt[(size_t)c * kBins + b];
-      if (by_bin) {
-#pragma unroll 4
-        for (int c = tid / kBins; c < C; c += kDraw / kBins) m += w.mass[(size_t)c * kBins + b];
-      }
-      if (n) atomicAdd(&sh.cnt[b], n);
-      if (m) atomicAdd((unsigned long long*)&sh.mass[b], (unsigned long long)m);
-      if (tid < C) atomicMin(&sh.min_list, w.head[tid].list_bin);
+    const uint32_t room = (uint32_t)(kCands / C);
+    const float inv_room = 1.0f / (float)room;
+#pragma unroll
+    for (int i = 0; i < kHeld; ++i) {
+      const uint32_t at = i * kDraw + tid, c = (uint32_t)(((float)at + 0.5f) * inv_room);  // at / room: exact under 2^13
+      held[i] = c < (uint32_t)C && at - c * room < sh.n_list[c] ? w.list[at] : 0;
     }
-    __syncthreads();
-    auto mass_prefix = [&]() {  // bins' masses to those through each bin
+    // counts, or counts and masses, of the keys >= floor through each bin
+    auto tally = [&](bool with_mass, uint64_t floor) {
+      __syncthreads();
+      uint64_t* mass = sh.more;                             // copies of the histogram, by lane
+      uint32_t* cnt = reinterpret_cast<uint32_t*>(sh.seg);
+      if (tid < kBins * kCopies) cnt[tid] = 0, mass[tid] = 0;
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < kHeld; ++i) {
+        if (held[i] < floor || held[i] == 0) continue;
+        const int b = bin_of(r.depth(held[i])) * kCopies + tid % kCopies;
+        atomicAdd(&cnt[b], 1u);
+        if (with_mass) {
+          const uint64_t g = r.mass(held[i]);
+          if (g) atomicAdd((unsigned long long*)&mass[b], (unsigned long long)g);
+        }
+      }
+      __syncthreads();
       if (wave == 0) {
-        const uint64_t m0 = sh.mass[2 * lane], m1 = sh.mass[2 * lane + 1];
-        const uint64_t x = wave_scan_u64(m0 + m1);
-        sh.mass[2 * lane] = x - m1;
-        sh.mass[2 * lane + 1] = x;
+        uint32_t c0 = 0, c1 = 0;
+        uint64_t m0 = 0, m1 = 0;
+#pragma unroll
+        for (int i = 0; i < kCopies; ++i) {
+          c0 += cnt[2 * lane * kCopies + i];
+          c1 += cnt[(2 * lane + 1) * kCopies + i];
+          m0 += mass[2 * lane * kCopies + i];
+          m1 += mass[(2 * lane + 1) * kCopies + i];
+        }
+        const uint32_t cx = (uint32_t)wave_scan_u64(c0 + c1);
+        const uint64_t mx = wave_scan_u64(m0 + m1);
+        sh.cnt[2 * lane] = cx - c1;
+        sh.cnt[2 * lane + 1] = cx;
+        sh.mass[2 * lane] = mx - m1;
+        sh.mass[2 * lane + 1] = mx;
       }
       __syncthreads();
     };
-    if (by_bin) mass_prefix();
-    const uint32_t valid = sh.cnt[kBins - 1];
-    const bool by_k = r.q.k < valid;
-    bool by_p = r.q.p < 1.0;
     auto first_bin = [&](auto before) {  // first bin, of the last at most, that is not `before`
       int lo = 0, hi = kBins - 1;
       while (lo < hi) {
@@ -532,74 +538,71 @@ __global__ __launch_bounds__(kDraw) void draw_kernel(SampleArgs a, int C, int ch
       }
       return lo;
     };
-    auto bin_by_mass = [&](double want) {
-      return first_bin([&](int b) { return sh.cnt[b] == 0 || (double)sh.mass[b] < want; });
+    // Whether the lists hold every token at or above a logit: a chunk's list ends at
+    // a half octave below its own largest. (Then the counts and masses of the keys
+    // down to it are the row's, too.)
+    auto complete = [&](float z) {
+      const bool ok = head.tokens == head.n_list || ordered_bits(z) > head.top ||
+                      bin_of(depth_of(z, from_ordered_bits(head.top), r.c4)) <= head.list_bin;
+      return __syncthreads_and(ok) != 0;
     };
-    // the deepest bin that can hold a kept token; min_p's is one more than its
-    // border's, whatever way that rounds
-    int deepest = kBins - 1;
-    if (r.q.min_p > 0.0) deepest = r.q.min_p < 1.0 ? min(kBins - 1, bin_of((float)(-2.0 * log2(r.q.min_p))) + 1) : 0;
-    int k_bin = 0;
-    if (by_k) {
-      k_bin = first_bin([&](int b) { return sh.cnt[b] < r.q.k; });
-      deepest = k_bin;
-    } else if (by_p && by_bin) {
-      const int b = bin_by_mass(r.q.p * (double)sh.mass[kBins - 1]);
-      if (b <= deepest) deepest = b;
-      else by_p = false;  // min_p ends before
-    } else if (by_p) {
-      deepest = kBins - 1;  // top-k that keeps all of a row with few tokens: their masses come from the keys
-    }
-    N = sh.cnt[deepest];
-    from_list = deepest <= sh.min_list && N <= kCands;
-    if (from_list) {
-      // candidates: the first keys of every chunk's list
-      uint32_t n = 0;
-      if (tid < C) n = w.cnt[(size_t)tid * kBins + deepest];
-      const uint64_t x = scan(n);
-      if (tid < C) sh.from[tid] = (uint32_t)(x - n);
-      if (tid == C) sh.from[C] = (uint32_t)x;
-      __syncthreads();
-      for (int c = wave; c < C; c += kDraw / 64) {
-        const uint32_t at = sh.from[c], m = sh.from[c + 1] - at;
-        for (uint32_t i = lane; i < m; i += 64) sh.cand[at + i] = w.list[(size_t)c * kList + i];
-      }
-      __syncthreads();
-    }
-    uint64_t all = by_bin ? sh.mass[kBins - 1] : 0;  // mass that top-p is a share of
-    if (by_p && !by_bin && from_list) {
-      // the bins' masses from the keys
-      for (uint32_t i = tid; i < N; i += kDraw) {
-        const uint64_t k = sh.cand[i];
-        atomicAdd((unsigned long long*)&sh.mass[bin_of(r.depth(k))], (unsigned long long)r.mass(k));
-      }
-      __syncthreads();
-      mass_prefix();
-      all = sh.mass[kBins - 1];
-    }
-    if (by_k) {
-      const uint64_t above = k_bin ? sh.cnt[k_bin - 1] : 0, above_mass = k_bin ? sh.mass[k_bin - 1] : 0;
-      if (from_list)
-        from_list = search_bin<false>(sh, scan, r, N, k_bin, (uint32_t)(sh.cnt[k_bin] - above), r.q.k, 0.0, above, above_mass, 0, &r.threshold, &all);
-      if (!from_list) r.threshold = search_row<false>(sh, scan, r, r.q.k, 0.0, 0);
-    }
-    if (by_p && !by_bin && !from_list) {
+    const bool whole = N == valid;  // every token is listed
+    // mass of the row's tokens at or above the threshold, from the row
+    auto row_mass = [&]() {
       uint64_t m = 0;
       for (int i = tid; i < r.V; i += kDraw) {
         const float z = clean(r.z[i]);
         if (z != -INFINITY && rank_key(z, i) >= r.threshold) m += mass_of(exponent_of(z, r.ref, r.q.c));
       }
       scan(m);
-      all = scan.sum;
-      __syncthreads();
-    }
-    if (by_p) {
-      const double want = r.q.p * (double)all;
+      return scan.sum;
+    };
+    from_list = true;
+    if (by_k) {
+      from_list = r.q.k <= N;
       if (from_list) {
-        const int b = bin_by_mass(want);
+        tally(false, 0);
+        const int b = first_bin([&](int i) { return sh.cnt[i] < r.q.k; });
+        const uint64_t above = b ? sh.cnt[b - 1] : 0;
+        from_list = search_bin<false>(sh, scan, r, held, b, (uint32_t)(sh.cnt[b] - above), r.q.k, 0.0, above, 0, 0, &r.threshold) &&
+                    complete(key_val(r.threshold));
+      }
+      if (!from_list) {
+        r.threshold = search_row<false>(sh, scan, r, r.q.k, 0.0, 0);
+        if (by_p) all = row_mass();
+      }
+    } else if (by_p && !of_all && !whole) {  // top-k that keeps all of a row with few tokens
+      from_list = false;
+      all = row_mass();
+    }
+    if (from_list && (by_p || (!by_k && r.q.min_p > 0.0))) {
+      tally(true, r.threshold);
+      if (!of_all) all = sh.mass[kBins - 1];
+    }
+    const double want = r.q.p * (double)all;
+    // min_p alone: its border, taken half an octave deeper, whatever way that rounds
+    bool by_min = false;
+    if (!by_k && r.q.min_p > 0.0 && from_list) {
+      const double depth = r.q.min_p < 1.0 ? -2.0 * log2(r.q.min_p) + 1.0 : 1.0;
+      const int b = bin_of((float)depth);
+      by_min = !by_p || (b < kBins - 1 && (double)sh.mass[b] < want);
+      if (by_min) {
+        const float z = (float)((double)r.ref - depth * 0.5 / r.q.c);
+        by_min = whole || (z > -INFINITY && complete(z));
+        if (by_min) by_p = false;  // top-p, if it is on, cuts deeper than min_p
+      }
+    }
+    if (!by_k && !by_p && !by_min) from_list = whole;  // nothing is cut
+    if (by_p) {
+      if (from_list) from_list = (double)sh.mass[kBins - 1] >= want;  // else it ends below the lists
+      if (from_list) {
+        const int b = first_bin([&](int i) { return sh.cnt[i] == 0 || (double)sh.mass[i] < want; });
         const uint64_t above = b ? sh.cnt[b - 1] : 0, above_mass = b ? sh.mass[b - 1] : 0;
-        uint64_t unused;
-        from_list = search_bin<true>(sh, scan, r, N, b, (uint32_t)(sh.cnt[b] - above), 0, want, above, above_mass, r.threshold, &r.threshold, &unused);
+        uint64_t key = 0;
+        from_list = search_bin<true>(sh, scan, r, held, b, (uint32_t)(sh.cnt[b] - above), 0, want, above, above_mass,
+                                     r.threshold, &key) &&
+                    (by_k || complete(key_val(key)));
+        if (from_list) r.threshold = key;
       }
       if (!from_list) r.threshold = search_row<true>(sh, scan, r, 0, want, r.threshold);
     }
@@ -608,9 +611,10 @@ __global__ __launch_bounds__(kDraw) void draw_kernel(SampleArgs a, int C, int ch
     __syncthreads();
     if (from_list) {
       uint64_t count = 0;
-      for (uint32_t i = tid; i < N; i += kDraw) {
-        const uint64_t k = sh.cand[i];
-        if (k < r.threshold) continue;
+#pragma unroll
+      for (int i = 0; i < kHeld; ++i) {
+        const uint64_t k = held[i];
+        if (k < r.threshold || k == 0) continue;
         const float z = key_val(k);
         const double t = exponent_of(z, r.ref, r.q.c);
         if (r.q.min_p > 0.0 && z != r.ref && exp2_64(t, 0) < r.q.min_p) continue;
@@ -621,21 +625,23 @@ __global__ __launch_bounds__(kDraw) void draw_kernel(SampleArgs a, int C, int ch
       n_kept = (uint32_t)scan.sum;
     }
   } else {
-    // the chunk from the chunks' masses
-    const uint64_t m = tid < C ? w.head[tid].mass : 0;
-    const uint64_t x = scan(m);
+    // the chunk from the chunks' masses, then the draw inside it, against its own
+    // largest logit, at the share of its mass that is left
+    const uint64_t m = chunk_mass, x = scan(m);
     total = scan.sum;
     const double want = r.q.u * (double)total;
     if (m && (double)x > want && !((double)(x - m) > want)) {
       sh.pick = tid;
       sh.above_mass = x - m;
+      sh.above = m;
+      sh.n = head.top;
     }
     __syncthreads();
     first_seg = (int)sh.pick * (chunk / kSeg);
     last_seg = min(n_seg, first_seg + chunk / kSeg);
-    before = sh.above_mass;
-    scan(tid < C ? w.head[tid].tokens : 0);
-    n_kept = (uint32_t)scan.sum;
+    part = fmin(fmax((want - (double)sh.above_mass) / (double)sh.above, 0.0), 1.0 - 0x1p-52);
+    r.ref = from_ordered_bits(sh.n);
+    n_kept = valid;
     for (int i = tid; i < n_seg; i += kDraw) sh.seg[i] = 0;
     __syncthreads();
   }
@@ -661,12 +667,13 @@ __global__ __launch_bounds__(kDraw) void draw_kernel(SampleArgs a, int C, int ch
   }
   __syncthreads();
   // the segment: thread t holds segments 2 t and 2 t + 1
+  double want;
   {
     const uint64_t s0 = 2 * tid < n_seg ? sh.seg[2 * tid] : 0;
     const uint64_t s1 = 2 * tid + 1 < n_seg ? sh.seg[2 * tid + 1] : 0;
-    const uint64_t x = before + scan(s0 + s1);
+    const uint64_t x = scan(s0 + s1);
     if (filtered) total = scan.sum;
-    const double want = r.q.u * (double)total;
+    want = part * (double)scan.sum;
     const uint64_t b1 = x - s1, b0 = b1 - s0;
     if (s0 && (double)b1 > want && !((double)b0 > want)) sh.pick = 2 * tid, sh.above_mass = b0;
     if (s1 && (double)x > want && !((double)b1 > want)) sh.pick = 2 * tid + 1, sh.above_mass = b1;
@@ -678,31 +685,24 @@ __global__ __launch_bounds__(kDraw) void draw_kernel(SampleArgs a, int C, int ch
   const int id = seg * kSeg + tid;
   const uint64_t m = tid < kSeg && id < r.V ? r.weight(id, kept) : 0;
   const uint64_t x = c0 + scan(m);
-  const double want = r.q.u * (double)total;
   if (m && (double)x > want && !((double)(x - m) > want)) {
     a.tok[row] = id;
     if (a.kept) a.kept[row] = (int32_t)n_kept;
     if (a.logp)
-      a.logp[row] = (float)(exponent_of(clean(r.z[id]), r.ref, r.q.c) * 0.6931471805599453 - log((double)total * 0x1p-43));
+      a.logp[row] = (float)(exponent_of(clean(r.z[id]), ref, r.q.c) * 0.6931471805599453 - log((double)total * 0x1p-43));
   }
 }
 
 }  // namespace
 
-// Never falls when an argument grows: fewer rows may take smaller chunks, but then
-// fewer than 4 * 256 in all.
-size_t sample_ws_bytes(int32_t rows, int32_t vocab) {
-  const int64_t few = std::min<int64_t>((int64_t)rows * chunks_of(kFew, vocab), 4 * 256);
-  return std::max(row_bytes(chunks_of(kMany, vocab)) * rows, row_bytes((int)few) + (size_t)16 * rows);
-}
+// Of the smaller chunks, whichever a call takes: never falls when an argument grows.
+size_t sample_ws_bytes(int32_t rows, int32_t vocab) { return row_bytes(chunks_of(kFew, vocab)) * rows; }
 
 hipError_t launch_sample(const SampleArgs& a, hipStream_t s) {
   const int each = each_of(a.rows, a.vocab), C = chunks_of(each, a.vocab);
   if (each == kFew) {
-    hipLaunchKernelGGL(top_kernel<kFew>, dim3(C, a.rows), dim3(kTally), 0, s, a);
     hipLaunchKernelGGL(tally_kernel<kFew>, dim3(C, a.rows), dim3(kTally), 0, s, a);
   } else {
-    hipLaunchKernelGGL(top_kernel<kMany>, dim3(C, a.rows), dim3(kTally), 0, s, a);
     hipLaunchKernelGGL(tally_kernel<kMany>, dim3(C, a.rows), dim3(kTally), 0, s, a);
   }
   hipLaunchKernelGGL(draw_kernel, dim3(a.rows), dim3(kDraw), 0, s, a, C, kTally * each);
