@@ -54,11 +54,11 @@ struct Work {
   uint64_t* list;
   Chunk* head;
 };
-// the larger chunks also where the smaller ones would be more than kMaxChunks
 inline int chunks_of(int each, int vocab) { return (vocab + kTally * each - 1) / (kTally * each); }
 inline int each_of(int rows, int vocab) {
-  return (int64_t)rows * chunks_of(kMany, vocab) < 256 && chunks_of(kFew, vocab) <= kMaxChunks ? kFew : kMany;
+  return (int64_t)rows * chunks_of(kMany, vocab) < 256 ? kFew : kMany;
 }
+static_assert(kMaxChunks * kTally * kFew == 1 << 20, "all chunks of the largest vocabulary");
 __host__ __device__ inline size_t row_bytes(int C) { return (kCands * 8 + (size_t)C * sizeof(Chunk) + 15) / 16 * 16; }
 __device__ __forceinline__ Work work_of(const SampleArgs& a, int row, int C) {
   char* p = static_cast<char*>(a.ws) + row_bytes(C) * row;
@@ -329,7 +329,7 @@ __device__ uint64_t search_row(Shared& sh, Scan& scan, const Row& r, uint64_t n,
   } else if (n - above < equal) {
     t = (uint32_t)(n - above);
   }
-  if (t == equal) return (uint64_t)prefix << 32;  // all of them
+  if (t == equal) return max((uint64_t)prefix << 32, floor);  // all of them
   // the t-th id: equal logits counted by blocks of kDraw ids
   uint32_t seen = 0;
   for (int i0 = 0; i0 < r.V; i0 += kDraw) {

@@ -96,6 +96,25 @@ def test_equal_logits(V):
         assert all(abs(x + math.log(kept)) <= 2.0 ** -22 * math.log(kept) + 1e-12 for x in logp)
 
 
+@pytest.mark.parametrize("V", [3000, 20000, 152064])
+def test_top_p_of_a_top_k_that_cuts_ties(V):
+    """top-k ends among equal logits and top-p keeps all of its tokens, or all but the last: no tie past k comes back.
+    Equal masses: p k is at least (k - 1) only for p >= 1 - 1 / k, so that fp32's 0.9999 keeps all of k = 2500 or fewer."""
+    z = torch.full((4, V), -0.5)
+    z[1:, ::7] = 0.75  # as many tokens as V / 7 lead
+    u = [0.0, 0.4, 0.8, 1.0 - 2.0 ** -24]
+    for k in (3, 400, 2500):
+        for p, less in ((0.9999, 0), (1.0 - 1.5 / k, 1)):
+            tok, _, n = sample(z[:1], u[2:3], k=k, p=p)
+            assert n == [k - less] and tok == [int(math.floor(float(torch.tensor(u[2], dtype=torch.float32)) * (k - less)))]
+    lead = (V + 6) // 7
+    k = min(300, lead - 1)
+    for p, less in ((0.9999, 0), (1.0 - 1.5 / k, 1)):
+        tok, _, n = sample(z[1:], u[1:], k=k, p=p)
+        assert n == [k - less] * 3
+        assert tok == [7 * int(math.floor(float(torch.tensor(x, dtype=torch.float32)) * (k - less))) for x in u[1:]]
+
+
 def test_masked_and_non_finite_logits():
     z = torch.full((6, 300), -math.inf)
     z[1, 5] = 0.0
