@@ -414,7 +414,7 @@ msd_status msd_reuse_select(const msd_model* model, const msd_block* block, cons
  * positions that a call touches; one outside [0, n_pages) sets MSD_DEV_PAGE
  * (append and commit: that block's rows are not stored; attention: its keys
  * are left out). Sequences may share pages that they only read. A block of
- * 16 tokens that one call writes belongs to one sequence.
+ * 16 tokens that one call writes is one place of one sequence's table.
  * Limits: head_dim in {64, 128}; page_size in {16, 32, 64, 128, 256};
  * max_pages * page_size <= 2^30.
  */
@@ -553,15 +553,17 @@ msd_status msd_verify_block_paged(const msd_model* model, const msd_paged_kv* kv
  *               tokens (ties to the smaller id) with mass >= top_p; one at
  *               least (top_p >= 1 or NaN: all);
  *  min_p        of those, tokens with p >= min_p * max p (min_p <= 0 or NaN:
- *               all; the most likely one always stays).
+ *               all; tokens as likely as the most likely always stay).
  * tok is the first id, ascending, whose cumulative mass over the kept tokens
  * exceeds u * total: the inverse CDF of msd_accept (u outside [0, 1) is
  * clamped to it). logp is its log-probability in the kept, renormalised law,
  * kept the number of kept tokens. A row without a logit above -inf gives
  * tok -1, logp -inf, kept 0.
- * Masses are 64-bit fixed point, 2^-43 of the most likely token's a step, from
- * fp64 exponentials: sums do not depend on their order, so the same inputs
- * give the same token on every run. Tokens under half a step draw nothing.
+ * Masses are 64-bit fixed point, from fp64 exponentials: a step is 2^-43 of the
+ * most likely token's mass (in sums over all tokens, of the most likely one's of
+ * some thousand consecutive ids, at most that). Sums do not depend on their
+ * order, so the same inputs give the same token on every run. Of filtered rows,
+ * tokens under half a step draw nothing.
  * With every block row sampled, tok is the argmax argument of msd_accept's
  * MSD_GREEDY walk: sample-and-compare (Sec. 3.1) under the filtered laws.
  */
