@@ -66,7 +66,7 @@ __global__ __launch_bounds__(256) void paged_merge_kernel(PagedAttnArgs a) {
 
 hipError_t launch_paged_attention(bool fp8, const PagedAttnArgs& a, const Topo& topo, hipStream_t s) {
   const int64_t wgs = (int64_t)(a.wgs > 0 ? a.wgs : a.batch) * a.kv.heads * a.groups;
-  if (wgs > 0x7FFFFFFF / 256 || a.q_per_wg < 1 || a.q_per_wg > paged_max_tiles(fp8, a.kv.head_dim) || (a.wgs > 0 && a.batch > kPagedPlanBatch))
+  if (wgs > 0x7FFFFFFF / 512 || a.q_per_wg < 1 || a.q_per_wg > paged_max_tiles(fp8, a.kv.head_dim) || (a.wgs > 0 && a.batch > kPagedPlanBatch))
     return hipErrorInvalidValue;
   const dim3 grid((uint32_t)wgs);
   if (a.kv.head_dim == 128) {

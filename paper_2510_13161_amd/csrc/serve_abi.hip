@@ -84,7 +84,8 @@ PagedShape paged_shape(const msd_paged_kv* kv, int32_t batch, int32_t n_slots, i
   s.groups = (tiles + most - 1) / most;
   s.q_per_wg = (tiles + s.groups - 1) / s.groups;
   const int64_t share = (s.q_per_wg == 1 && light ? kPagedWgs : kPagedWgsMany) / ((int64_t)heads * s.groups);
-  s.wgs = blocks <= kPagedAlone || share <= batch || batch > kPagedPlanBatch
+  // (the plan counts all sequences' blocks in 32 bits)
+  s.wgs = blocks <= kPagedAlone || share <= batch || batch > kPagedPlanBatch || blocks * batch > INT32_MAX
               ? 0
               : (int)std::min<int64_t>(share, batch * ((blocks + 7) / 8));
   return s;

@@ -193,12 +193,26 @@ def _fits(kv, rows) -> None:
     heads, hd = getattr(rows, "_heads", (None, kv.head_dim))
     if heads not in (None, kv.n_kv_heads) or hd != kv.head_dim:
         _need(False, "rows and pages differ in kv heads or head_dim")
+    _here(kv, rows)
+
+
+def _here(*structs) -> None:
     here = torch.cuda.current_device()
-    if getattr(kv, "_device", here) != here or getattr(rows, "_device", here) != here:
-        _need(False, "tensors of another device than the current one")
+    for s in structs:
+        if s is not None and getattr(s, "_device", here) != here:
+            _need(False, "tensors of another device than the current one")
+
+
+def _one_device(*tensors) -> int:
+    """The device of a call's tensors (None: absent), which has to be one."""
+    at = {t.get_device() for t in tensors if t is not None}
+    _need(len(at) == 1 and min(at) >= 0, "tensors of several devices, or of the host")
+    return at.pop()
 
 
 def _nbytes(ws: torch.Tensor) -> int:
+    _need(ws.get_device() == torch.cuda.current_device() and ws.is_contiguous(),
+          "workspace: a contiguous tensor of the current device")
     return ws.numel() * ws.element_size()
 
 
@@ -316,6 +330,8 @@ def set_profile(handle, kclass: int, begin_events, end_events) -> None:
 
 def paged_append(kv: PagedKV, rows: KVRows, rope: Optional[Rope] = None, stream=None) -> None:
     _fits(kv, rows)
+    if rope is not None:
+        _here(rope)
     _check(lib().msd_paged_append(ctypes.byref(kv), ctypes.byref(rows),
                                   ctypes.byref(rope) if rope is not None else None,
                                   _stream(stream)))
@@ -325,8 +341,10 @@ def paged_commit(kv: PagedKV, rows: KVRows, acc_len, path, rope: Optional[Rope] 
                  stream=None) -> None:
     """acc_len: device int32 [batch], path: device int32 [batch][n_rows], as accept wrote them."""
     _fits(kv, rows)
+    _here(rope)
     _typed(acc_len, torch.int32, (rows.batch,), "acc_len")
     _typed(path, torch.int32, (rows.batch, rows.n_rows), "path")
+    _need(_one_device(acc_len, path) == torch.cuda.current_device(), "tensors of another device than the current one")
     _check(lib().msd_paged_commit(ctypes.byref(kv), ctypes.byref(rows),
                                   ctypes.byref(rope) if rope is not None else None, _ptr(acc_len),
                                   _ptr(path), _stream(stream)))
@@ -353,6 +371,9 @@ def verify_block_paged(handle, kv: PagedKV, block: Block, ee: Optional[EERequest
     shape = (kv.n_layers, block.batch, kv.n_kv_heads, block.n_slots, kv.head_dim)
     _typed(k_rows, torch.bfloat16, shape, "k_rows")
     _typed(v_rows, torch.bfloat16, shape, "v_rows")
+    _need(_one_device(k_rows, v_rows, logits, argmax, lse) == torch.cuda.current_device(),
+          "tensors of another device than the current one")
+    _here(kv)
     _check(lib().msd_verify_block_paged(handle, ctypes.byref(kv), ctypes.byref(block),
                                         ctypes.byref(ee) if ee is not None else None, _ptr(k_rows), _ptr(v_rows),
                                         int(window), int(sinks), _ptr(logits), _ptr(argmax), _ptr(lse), _ptr(ws),
@@ -377,7 +398,8 @@ def sample(logits: torch.Tensor, u: torch.Tensor, params: Optional[SampleParams]
     if kept is not None:
         _typed(kept, torch.int32, (rows,), "kept")
     _need(params is None or getattr(params, "_rows", None) in (None, rows), "params: one value for each row of logits")
-    _need(logits.device.index == torch.cuda.current_device(), "tensors of another device than the current one")
+    _need(_one_device(logits, u, tok, logp, kept) == torch.cuda.current_device(), "tensors of another device than the current one")
+    _here(params)
     _check(lib().msd_sample(logits.data_ptr(), logits.stride(0) if rows > 1 else vocab, rows, vocab,
                             ctypes.byref(params) if params is not None else None, _ptr(u), _ptr(tok),
                             _ptr(logp), _ptr(kept), _ptr(ws), _nbytes(ws), _stream(stream)))
@@ -487,7 +509,7 @@ class PagedCache:
                          _ptr(status), MSD_KV_FP8 if fp8 else MSD_KV_BF16, L, pages, heads, page, hd,
                          batch_cap, max_pages)
         self.c._keep = (k, v, k_scale, v_scale, page_table, len, status)
-        self.c._device = k.device.index
+        self.c._device = _one_device(k, v, k_scale, v_scale, page_table, len, status)
 
     @staticmethod
     def allocate(n_layers: int, n_kv_heads: int, head_dim: int, n_pages: int, page_size: int,
@@ -511,6 +533,7 @@ def rope(table: torch.Tensor, layout: str = "half") -> Rope:
     _typed(table, torch.float32, table.shape, "table")
     r = Rope(_ptr(table), table.shape[0], 2 * table.shape[1], ROPE_LAYOUTS[layout])
     r._keep = (table,)
+    r._device = _one_device(table)
     return r
 
 
@@ -534,7 +557,7 @@ def kv_rows(k: torch.Tensor, v: torch.Tensor, layer: int = 0, count: Optional[to
         _typed(count, torch.int32, (k.shape[1],), "count")
     r = KVRows(k.data_ptr(), v.data_ptr(), *st, layer, k.shape[0], k.shape[1], k.shape[2], _ptr(count))
     r._keep = (k, v, count)
-    r._heads, r._device = tuple(k.shape[3:]), k.device.index
+    r._heads, r._device = tuple(k.shape[3:]), _one_device(k, v, count)
     return r
 
 
@@ -552,6 +575,7 @@ def paged_attn(q: torch.Tensor, out: torch.Tensor, k_new: Optional[torch.Tensor]
     _need(q.dim() == 4 and q.shape == out.shape, "q and out: [batch][slots][heads][head_dim]")
     B, n, H, hd = q.shape
     qs, os_ = _strided(q, "q"), _strided(out, "out")
+    _need(all(st > 0 for st, size in zip(out.stride(), out.shape) if size > 1), "out: no row twice")
     _need((k_new is None) == (v_new is None), "k_new and v_new go together")
     ns = [0, 0, 0]
     if k_new is not None:
@@ -571,7 +595,7 @@ def paged_attn(q: torch.Tensor, out: torch.Tensor, k_new: Optional[torch.Tensor]
                   ctypes.pointer(rope) if rope is not None else None,
                   float(hd) ** -0.5 if scale is None else float(scale), B, n, H, int(window), int(sinks))
     a._keep = (q, out, k_new, v_new, arr, count, rope)
-    a._heads, a._device = (None if k_new is None else k_new.shape[2], hd), q.device.index
+    a._heads, a._device = (None if k_new is None else k_new.shape[2], hd), _one_device(q, out, k_new, v_new, count, *(rope._keep if rope is not None else ()))
     return a
 
 
@@ -586,5 +610,7 @@ def sample_params(temperature: Optional[torch.Tensor] = None, top_k: Optional[to
             _typed(t, dt, (rows,), what)
     p = SampleParams(_ptr(temperature), _ptr(top_k), _ptr(top_p), _ptr(min_p))
     p._rows = rows
+    if rows is not None:
+        p._device = _one_device(temperature, top_k, top_p, min_p)
     p._keep = (temperature, top_k, top_p, min_p)
     return p

@@ -464,6 +464,67 @@ def test_attention_strides_streams_and_scale():
     assert bool((buf[:, :, 0] == 7.0).all()) and bool((buf[:, :, n + 1] == 7.0).all())
 
 
+@pytest.mark.parametrize("fmt,hd", [("bf16", 128), ("fp8", 64), ("fp8", 128)])
+def test_scale_of_zero_weighs_all_seen_keys_alike(fmt, hd):
+    lens, n, H, Hk = [700, 9, 0], 4, 4, 2
+    c = make_cache(fmt, 1, Hk, hd, 64, lens, n, 8)
+    g = gen(16)
+    q, kn, vn = normal(g, 3, n, H, hd), normal(g, 3, n, Hk, hd), normal(g, 3, n, Hk, hd)
+    for window in (0, 50):
+        out = run_attention(c, q, kn, vn, parent=[-1, 0, 0, 1], window=window, sinks=3, scale=0.0)
+        check(out, *reference(c, 0, q, kn, vn, lens, [-1, 0, 0, 1], None, None, "half", window, 3, 0.0))
+
+
+def test_windows_and_sinks_past_every_position_keep_all_keys():
+    lens, n = [900, 33], 3
+    c = make_cache("fp8", 1, 2, 128, 64, lens, n, 21)
+    g = gen(17)
+    q, kn, vn = normal(g, 2, n, 4, 128), normal(g, 2, n, 2, 128), normal(g, 2, n, 2, 128)
+    want = run_attention(c, q, kn, vn)
+    for window, sinks in ((2 ** 31 - 1, 0), (2 ** 31 - 1, 2 ** 31 - 1), (1, 2 ** 31 - 1)):
+        got = run_attention(c, q, kn, vn, window=window, sinks=sinks)
+        check(got, *reference(c, 0, q, kn, vn, lens, [-1, 0, 1], None, None, "half", 0, 0, 128 ** -0.5))
+        assert window == 1 or bool((got == want).all())
+
+
+def test_calls_on_two_streams_at_once():
+    """Workspaces of their own, one cache that both read: each result is that of the call alone."""
+    lens, n = [3000, 40, 1200], 5
+    c = make_cache("fp8", 1, 2, 128, 64, lens, n, 22)
+    g = gen(18)
+    qs = [normal(g, 3, n, 8, 128).cuda() for _ in range(2)]
+    kn, vn = normal(g, 3, n, 2, 128).cuda(), normal(g, 3, n, 2, 128).cuda()
+    want = [run_attention(c, q, kn, vn) for q in qs]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    nb = msd.paged_attention_workspace_bytes(c.c, 3, n, 8)
+    ws = [torch.empty(nb, dtype=torch.uint8, device="cuda") for _ in range(2)]
+    out = [[torch.empty_like(q) for _ in range(8)] for q in qs]
+    for s in streams:
+        s.wait_stream(torch.cuda.current_stream())
+    for r in range(8):
+        for i, s in enumerate(streams):
+            msd.paged_attention(c.c, 0, msd.paged_attn(qs[i], out[i][r], kn, vn), ws[i], stream=s)
+    torch.cuda.synchronize()
+    assert all(bool((o == want[i]).all()) for i in range(2) for o in out[i])
+
+
+def test_binding_refuses_host_workspaces_and_outputs_that_overlap():
+    c = make_cache("bf16", 1, 2, 64, 16, [4], 2, 1)
+    x = torch.zeros(1, 2, 2, 64, dtype=torch.bfloat16, device="cuda")
+    a = msd.paged_attn(x, torch.empty_like(x), x, x)
+    nb = msd.paged_attention_workspace_bytes(c.c, 1, 2, 2)
+    with pytest.raises((msd.MsdError, AssertionError)):
+        msd.paged_attention(c.c, 0, a, torch.empty(nb, dtype=torch.uint8))
+    with pytest.raises(msd.MsdError):
+        msd.paged_attn(x, x[:, :1].expand(1, 2, 2, 64), x, x)
+    with pytest.raises(msd.MsdError):
+        msd.paged_commit(c.c, msd.kv_rows(x, x), torch.zeros(1, dtype=torch.int32), torch.zeros(1, 2, dtype=torch.int32))
+    z = torch.zeros(2, 5, device="cuda")
+    u, tok = torch.zeros(2, device="cuda"), torch.zeros(2, dtype=torch.int32, device="cuda")
+    with pytest.raises((msd.MsdError, AssertionError)):
+        msd.sample(z, u, None, tok, torch.empty(msd.sample_workspace_bytes(2, 5), dtype=torch.uint8))
+
+
 def test_binding_refuses_rows_of_another_cache():
     c = make_cache("bf16", 1, 2, 64, 16, [4], 2, 1)
     x = torch.zeros(1, 2, 4, 64, dtype=torch.bfloat16, device="cuda")
