@@ -10,9 +10,10 @@
 //  1 tally  a workgroup a chunk of 8192 logits, held in registers: the largest; where
 //           the row needs the mass of all tokens (unfiltered, or top-p without
 //           top-k) the chunk's, against its own largest; for filtered rows the
-//           chunk's highest tokens: a histogram of counts over half octaves below its
-//           largest says how many half octaves fit the chunk's share of
-//           4096 keys, and those are listed.
+//           chunk's highest tokens. A histogram over half octaves below its largest, of
+//           the threads' largest logits, bounds what fits the chunk's share of 4096 keys;
+//           the tokens above that bound are put together (most end here), a histogram of
+//           those says how many half octaves fit, and these are listed.
 //  2 draw   a workgroup a row, the lists in its registers. A cut is found by a histogram of
 //           counts and masses over half octaves below the row's largest, then over
 //           1024 parts of one half octave, then by ranking the few keys of one
@@ -21,9 +22,15 @@
 //           searched digit by digit over the row. The draw: masses of 512-id
 //           segments, the segment, the id. Unfiltered rows take the chunk from the
 //           chunks' masses.
-// The logits are read once: 144 rows of 152K are 87.6 MB.
+// The logits are read once: 144 rows of 152K are 87 MB, 18 us for a kernel that does no
+// more than read them (4.9 TB/s). The tally takes 28 us, the fp64 masses, where a row needs
+// them, 6 to 16 more: the chunks of a dispatch round are loaded together and worked on
+// together, so their times add. (A chunk's loads issued while the one before is worked
+// on: 40 us, at half the waves.) The draw is a chain of some 20 barriers: 9 us unfiltered,
+// 11 for one filter, 15 for all, 24 for 144 rows of top-1000 with top-p.
 #include <algorithm>
 
+#include "paged.h"
 #include "sample.h"
 
 namespace msd {
@@ -70,7 +77,7 @@ __device__ __forceinline__ Work work_of(const SampleArgs& a, int row, int C) {
 // inside the bin is the fraction.
 __device__ __forceinline__ float depth_of(float z, float ref, float c4) { return (0.5f * ref - 0.5f * z) * c4; }
 __device__ __forceinline__ int bin_of(float x) { return (int)fminf(x, (float)(kBins - 1)); }
-__device__ __forceinline__ float c4_of(const Request& q) { return (float)fmin(4.0 * q.c, 3e38); }
+__device__ __forceinline__ float c4_of(const Request& q) { return (float)fmin(q.c / 8, 3e38); }
 // whether top-p is a share of the mass of tokens that no list may hold
 __device__ __forceinline__ bool share_of_all(const Request& q, int V) { return q.p < 1.0 && q.k >= (uint32_t)V; }
 
@@ -103,30 +110,33 @@ __device__ __forceinline__ uint64_t lane_u64(uint64_t v, int lane) {
 }
 __device__ __forceinline__ uint64_t wave_sum_u64(uint64_t v) { return lane_u64(wave_scan_u64(v), 63); }
 
-// Four consecutive logits, cleaned, those past the row as -inf. Rows start at any
+// Four consecutive logits, bounded, those past the row as -inf. Rows start at any
 // fp32 (a 16-byte load takes any 4-byte address).
 typedef float float4_any __attribute__((ext_vector_type(4), aligned(4)));
 __device__ __forceinline__ void load4(const float* z, int i, int V, float* v) {
   if (i + 4 <= V) {
     const float4_any x = *reinterpret_cast<const float4_any*>(z + i);
 #pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] = clean(x[e]);
+    for (int e = 0; e < 4; ++e) v[e] = bounded(x[e]);
   } else {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] = i + e < V ? clean(z[i + e]) : -INFINITY;
+    for (int e = 0; e < 4; ++e) v[e] = i + e < V ? bounded(z[i + e]) : -INFINITY;
   }
 }
 
-constexpr int kCopies = 4;  // of the histogram, by lane: tokens of one bin meet less often
+constexpr int kCopies = 4;     // of the histogram, by lane: tokens of one bin meet less often
+constexpr int kPicked = 1024;  // tokens of a chunk that may be listed, at most
 template <int EACH>
-__global__ __launch_bounds__(kTally) void tally_kernel(SampleArgs a) {
+__global__ __launch_bounds__(kTally, 8) void tally_kernel(SampleArgs a) {
+  constexpr int kWaves = kTally / 64;
+  __shared__ double parts[32];
+  __shared__ uint2 picked[kPicked];  // logit, id
   __shared__ uint32_t cnt[kBins * kCopies];
   __shared__ uint32_t cursor[kBins];
-  __shared__ uint64_t red[kTally / 64];
-  __shared__ uint32_t red_n[kTally / 64], red_top[kTally / 64];
-  __shared__ uint32_t last_bin;
-  __shared__ int list_bin;
-  const int C = gridDim.x, c = blockIdx.x, row = blockIdx.y, tid = threadIdx.x;
+  __shared__ uint64_t red[kWaves];
+  __shared__ uint32_t red_n[kWaves], red_top[kWaves], red_in[kWaves];
+  __shared__ int limit, list_bin;
+  const int C = gridDim.x, c = blockIdx.x, row = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const Work w = work_of(a, row, C);
   const float* z = a.logits + (int64_t)row * a.row_stride;
   const int first = c * (kTally * EACH) + 4 * tid;  // v[j]: id first + kTally * (j & ~3) + (j & 3)
@@ -135,15 +145,15 @@ __global__ __launch_bounds__(kTally) void tally_kernel(SampleArgs a) {
   for (int j = 0; j < EACH; j += 4) load4(z, first + j * kTally, a.vocab, v + j);
   const Request q = request_of(a, row);
   for (int i = tid; i < kBins * kCopies; i += kTally) cnt[i] = 0;
-  if (tid == 0) last_bin = 0;
+  if (tid < 32) parts[tid] = octave_part(tid);
   float most = v[0];
 #pragma unroll
   for (int j = 1; j < EACH; ++j) most = fmaxf(most, v[j]);
-  uint32_t top = wave_max_u32(ordered_bits(most));
-  if ((tid & 63) == 0) red_top[tid >> 6] = top;
+  uint32_t top = wave_max_u32(ordered_bits(most + 0.0f));
+  if (lane == 0) red_top[wave] = top;
   __syncthreads();
 #pragma unroll
-  for (int i = 0; i < kTally / 64; ++i) top = max(top, red_top[i]);
+  for (int i = 0; i < kWaves; ++i) top = max(top, red_top[i]);
   if (top <= kDead) {
     if (tid == 0) w.head[c] = Chunk{kDead, kBins - 1, 0, 0, 0};
     return;
@@ -151,56 +161,113 @@ __global__ __launch_bounds__(kTally) void tally_kernel(SampleArgs a) {
   const float ref = from_ordered_bits(top);
   const float c4 = c4_of(q);
   const bool filtered = q.filtered(), need_mass = !filtered || share_of_all(q, a.vocab);
-  uint64_t sum = 0;
-  uint32_t tokens = 0;
-  uint32_t low = 0;  // tokens of the last bin, which most tokens of cold laws share
-  const int copy = tid % kCopies;
-#pragma unroll
-  for (int j = 0; j < EACH; ++j) {
-    if (v[j] == -INFINITY) continue;
-    ++tokens;
-    if (need_mass) sum += mass_of(exponent_of(v[j], ref, q.c));
-    if (!filtered) continue;
-    const int b = bin_of(depth_of(v[j], ref, c4));
-    if (b == kBins - 1) ++low;
-    else atomicAdd(&cnt[b * kCopies + copy], 1u);
-  }
-  sum = wave_sum_u64(sum);
-  tokens = (uint32_t)wave_sum_u64(tokens);
-  if (low) atomicAdd(&last_bin, low);
-  if ((tid & 63) == 0) red[tid >> 6] = sum, red_n[tid >> 6] = tokens;
-  __syncthreads();
   const uint32_t room = (uint32_t)(kCands / C);
-  if (tid < 64) {
-    // counts through each bin; the deepest bin down to which they fit the list
+  const int copy = tid % kCopies;
+  auto bin = [&](float x) { return bin_of(depth_of(x, ref, c4)); };
+  // (a wave) this lane's two bins' counts through each, and how many bins fit the list
+  auto bins_that_fit = [&](uint32_t& x0, uint32_t& x1) {
     uint32_t c0 = 0, c1 = 0;
 #pragma unroll
-    for (int k = 0; k < kCopies; ++k) c0 += cnt[2 * tid * kCopies + k], c1 += cnt[(2 * tid + 1) * kCopies + k];
-    if (tid == 63) c1 = last_bin;
-    const uint32_t x = (uint32_t)wave_scan_u64(c0 + c1);
-    const unsigned long long f0 = __ballot(x - c1 <= room), f1 = __ballot(x <= room);
-    const int f = (int)__popcll(f0) + (int)__popcll(f1);
-    cursor[2 * tid] = x - c1 - c0;
-    cursor[2 * tid + 1] = x - c1;
+    for (int k = 0; k < kCopies; ++k) c0 += cnt[2 * lane * kCopies + k], c1 += cnt[(2 * lane + 1) * kCopies + k];
+    x1 = (uint32_t)wave_scan_add((int)(c0 + c1));
+    x0 = x1 - c1;
+    return (int)__popcll(__ballot(x0 <= room)) + (int)__popcll(__ballot(x1 <= room));
+  };
+  // First the threads' largest alone: a half octave through which they are more than
+  // the list holds cannot be listed, nor any below. Most tokens lie there, and are
+  // done with after one comparison.
+  if (filtered) {
+    if (most > -INFINITY) atomicAdd(&cnt[bin(most) * kCopies + copy], 1u);
+    __syncthreads();
+    if (wave == 0) {
+      uint32_t x0, x1;
+      const int f = bins_that_fit(x0, x1);
+      if (lane == 0) limit = f;
+#pragma unroll
+      for (int k = 0; k < 2 * kCopies; ++k) cnt[2 * lane * kCopies + k] = 0;
+    }
+  }
+  uint64_t sum = 0;
+  if (need_mass)
+#pragma unroll
+    for (int j = 0; j < EACH; ++j)
+      if (v[j] != -INFINITY) sum += mass_of(parts, exponent_of(v[j], ref, q.c));
+  uint32_t tokens = 0;  // of the wave
+#pragma unroll
+  for (int j = 0; j < EACH; ++j) tokens += (uint32_t)__popcll(__ballot(v[j] != -INFINITY));
+  if (need_mass) sum = wave_sum_u64(sum);
+  if (lane == 0) red[wave] = sum, red_n[wave] = tokens;
+  __syncthreads();
+  const int end = filtered ? limit : 0;
+  // below any logit of a half octave before `end`: one half octave deeper, and the rounding of that
+  float border = ref - 2.0f * (float)(end + 1) / c4;
+  border = end == kBins ? -INFINITY : border - fabsf(border) * 0x1p-22f;
+  uint32_t in = 0;
+  if (filtered) {
+#pragma unroll
+    for (int j = 0; j < EACH; ++j) in += (uint32_t)__popcll(__ballot(v[j] >= border && v[j] != -INFINITY));
+    if (lane == 0) red_in[wave] = in;
+  }
+  __syncthreads();
+  uint32_t n_in = 0, at = 0;
+  if (filtered) {
+#pragma unroll
+    for (int i = 0; i < kWaves; ++i) n_in += red_in[i], at += i < wave ? red_in[i] : 0;
+  }
+  const bool few = n_in <= kPicked;  // else (lists that hold most of a short row) all are looked at again
+  if (few && n_in) {
+#pragma unroll
+    for (int j = 0; j < EACH; ++j) {
+      const bool is = v[j] >= border && v[j] != -INFINITY;
+      const uint64_t mask = __ballot(is);
+      const uint32_t before = __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0u));
+      if (is) picked[at + before] = make_uint2(__float_as_uint(v[j]), (uint32_t)(first + kTally * (j & ~3) + (j & 3)));
+      at += (uint32_t)__popcll(mask);
+    }
+  }
+  __syncthreads();
+  // each token that may be listed to f(logit, id, half octave)
+  auto each_in = [&](auto f) {
+    if (few) {
+#pragma unroll
+      for (int i = 0; i < kPicked / kTally; ++i)
+        if (i * kTally + tid < (int)n_in) {
+          const uint2 x = picked[i * kTally + tid];
+          f(__uint_as_float(x.x), (int)x.y, bin(__uint_as_float(x.x)));
+        }
+    } else {
+#pragma unroll
+      for (int j = 0; j < EACH; ++j)
+        if (v[j] >= border && v[j] != -INFINITY) f(v[j], first + kTally * (j & ~3) + (j & 3), bin(v[j]));
+    }
+  };
+  if (filtered)
+    each_in([&](float, int, int b) {
+      if (b < end) atomicAdd(&cnt[b * kCopies + copy], 1u);
+    });
+  __syncthreads();
+  if (wave == 0) {
+    // counts through each bin; the deepest bin down to which they fit the list
+    uint32_t x0, x1;
+    const int f = min(bins_that_fit(x0, x1), end);
+    const uint32_t before = (uint32_t)__shfl_up((int)x1, 1);
+    cursor[2 * lane] = lane ? before : 0u;
+    cursor[2 * lane + 1] = x0;
     // tokens through the last bin that fits, bin f - 1 (lane (f - 1) / 2's second or first)
-    const uint32_t through = f & 1 ? x - c1 : x;
-    const uint32_t n_list = f ? (uint32_t)__builtin_amdgcn_readlane((int)through, (f - 1) >> 1) : 0u;
-    if (tid == 0) {
+    const uint32_t n_list = f ? (uint32_t)__builtin_amdgcn_readlane((int)(f & 1 ? x0 : x1), (f - 1) >> 1) : 0u;
+    if (lane == 0) {
       list_bin = f - 1;
       uint64_t s = red[0], n = red_n[0];
-      for (int i = 1; i < kTally / 64; ++i) s += red[i], n += red_n[i];
-      w.head[c] = Chunk{top, f - 1, filtered ? n_list : 0u, (uint32_t)n, s};
+      for (int i = 1; i < kWaves; ++i) s += red[i], n += red_n[i];
+      w.head[c] = Chunk{top, f - 1, n_list, (uint32_t)n, s};
     }
   }
   if (!filtered) return;
   __syncthreads();
   const int lb = list_bin;
-#pragma unroll
-  for (int j = 0; j < EACH; ++j) {
-    const int b = v[j] == -INFINITY ? kBins : bin_of(depth_of(v[j], ref, c4));
-    if (b <= lb)
-      w.list[(size_t)c * room + atomicAdd(&cursor[b], 1u)] = rank_key(v[j], first + kTally * (j & ~3) + (j & 3));
-  }
+  each_in([&](float x, int id, int b) {
+    if (b <= lb) w.list[(size_t)c * room + atomicAdd(&cursor[b], 1u)] = rank_key(x + 0.0f, id);
+  });
 }
 
 constexpr int kHeld = kCands / kDraw;  // keys of a thread
@@ -215,6 +282,8 @@ struct Shared {
   uint32_t top[kDraw / 64];
   uint32_t n, m, pick;
   uint32_t n_list[kMaxChunks];
+  uint32_t rank[kDraw];
+  double parts[32];
 };
 static_assert(kBins * kCopies <= kDraw, "a thread for each bin of the copies");
 static_assert(kSegs >= kDigit && 2 * kDraw >= kDigit, "masses and counts of the digits");
@@ -244,17 +313,19 @@ struct Row {
   uint32_t top;
   float c4;
   Request q;
+  const double* parts; // of an octave
   uint64_t threshold;  // smallest kept key
-  __device__ uint64_t mass(uint64_t key) const { return mass_of(exponent_of(key_val(key), ref, q.c)); }
+  __device__ uint64_t mass_at(float x) const { return mass_of(parts, exponent_of(x, ref, q.c)); }
+  __device__ uint64_t mass(uint64_t key) const { return mass_at(key_val(key)); }
   __device__ float depth(uint64_t key) const { return depth_of(key_val(key), ref, c4); }
   __device__ uint64_t weight(int i, bool& kept) const {
     const float x = clean(z[i]);
     kept = false;
     if (x == -INFINITY || rank_key(x, i) < threshold) return 0;
     const double t = exponent_of(x, ref, q.c);
-    if (q.min_p > 0.0 && x != ref && exp2_64(t, 0) < q.min_p) return 0;
+    if (q.min_p > 0.0 && x != ref && exp2_64(parts, t) < q.min_p) return 0;
     kept = true;
-    return mass_of(t);
+    return mass_of(parts, t);
   }
 };
 
@@ -283,7 +354,7 @@ __device__ uint64_t search_row(Shared& sh, Scan& scan, const Row& r, uint64_t n,
       const uint32_t d = (k >> shift) & ((1u << bits) - 1);
       atomicAdd(&cnt[d], 1u);
       if (BY_MASS) {
-        const uint64_t m = mass_of(exponent_of(z, r.ref, r.q.c));
+        const uint64_t m = r.mass_at(z);
         if (m) atomicAdd((unsigned long long*)&mass[d], (unsigned long long)m);
       }
     }
@@ -319,7 +390,7 @@ __device__ uint64_t search_row(Shared& sh, Scan& scan, const Row& r, uint64_t n,
   // of the `equal` tokens with this logit, the first t ids
   uint32_t t = equal;
   if (BY_MASS) {
-    const uint64_t one = mass_of(exponent_of(from_ordered_bits(prefix), r.ref, r.q.c));
+    const uint64_t one = r.mass_at(from_ordered_bits(prefix));
     uint32_t lo = 0;  // smallest t >= 1 with above_mass + t * one >= want, at most equal
     while (lo + 1 < t) {
       const uint32_t mid = (lo + t) / 2;
@@ -394,6 +465,7 @@ __device__ __forceinline__ bool search_bin(Shared& sh, Scan& scan, const Row& r,
     __syncthreads();
   }
   uint64_t* mine = sh.seg;
+  sh.rank[tid] = 0;
 #pragma unroll
   for (int i = 0; i < kHeld; ++i) {
     const int p = part_of(held[i]);
@@ -402,9 +474,19 @@ __device__ __forceinline__ bool search_bin(Shared& sh, Scan& scan, const Row& r,
   __syncthreads();
   const uint32_t m = sh.n;
   const uint64_t key = tid < (int)m ? mine[tid] : 0;
-  uint32_t rank = 0;
+  {
+    // a wave 64 of the keys against its part of all: as many parts as waves are left
+    const int wave = tid >> 6, groups = max(((int)m + 63) >> 6, 1), parts = kDraw / 64 / groups;
+    const int x = wave % groups * 64 + (tid & 63), part = wave / groups;
+    const uint64_t k = x < (int)m ? mine[x] : ~0ull;
+    const int each = ((int)m + parts - 1) / parts, end = min((int)m, (part + 1) * each);
+    uint32_t above_k = 0;
 #pragma unroll 8
-  for (uint32_t i = 0; i < m; ++i) rank += mine[i] > key;
+    for (int i = part * each; i < end; ++i) above_k += mine[i] > k;
+    if (above_k && part < parts) atomicAdd(&sh.rank[x], above_k);
+  }
+  __syncthreads();
+  const uint32_t rank = sh.rank[tid];
   if (!BY_MASS) {  // the token of rank n - 1, or the last
     const uint64_t last = n - above < m ? n - above : m;
     if (tid < (int)m && rank == last - 1) sh.key = key;
@@ -441,6 +523,8 @@ __global__ __launch_bounds__(kDraw) void draw_kernel(SampleArgs a, int C, int ch
   r.z = a.logits + (int64_t)row * a.row_stride;
   r.V = a.vocab;
   r.q = request_of(a, row);
+  r.parts = sh.parts;
+  if (tid < 32) sh.parts[tid] = octave_part(tid);
   const Chunk head = tid < C ? w.head[tid] : Chunk{kDead, kBins - 1, 0, 0, 0};
   {
     const uint32_t top = wave_max_u32(head.top);
@@ -472,8 +556,9 @@ __global__ __launch_bounds__(kDraw) void draw_kernel(SampleArgs a, int C, int ch
 
   // the chunks' masses against the row's largest
   const double down = head.top > kDead ? exponent_of(from_ordered_bits(head.top), r.ref, r.q.c) : 0.0;
-  const uint64_t chunk_mass = head.mass ? (uint64_t)((double)head.mass * exp2_64(down, 0) + 0.5) : 0;
-  const uint32_t valid = (uint32_t)(scan(head.tokens), scan.sum);
+  const uint64_t chunk_mass = head.mass ? (uint64_t)((double)head.mass * exp2_64(sh.parts, down) + 0.5) : 0;
+  const uint64_t counts = (scan((uint64_t)head.n_list << 32 | head.tokens), scan.sum);  // both under 2^21
+  const uint32_t valid = (uint32_t)counts, N = (uint32_t)(counts >> 32);  // tokens above -inf, listed ones
 
   uint64_t held[kHeld];  // listed keys of this thread, 0: none
   if (filtered) {
@@ -481,8 +566,6 @@ __global__ __launch_bounds__(kDraw) void draw_kernel(SampleArgs a, int C, int ch
     bool by_p = r.q.p < 1.0;
     uint64_t all = 0;  // mass that top-p is a share of
     if (of_all) scan(chunk_mass), all = scan.sum;
-    scan(head.n_list);
-    const uint32_t N = (uint32_t)scan.sum;
     if (tid < C) sh.n_list[tid] = head.n_list;
     __syncthreads();
     const uint32_t room = (uint32_t)(kCands / C);
@@ -552,7 +635,7 @@ __global__ __launch_bounds__(kDraw) void draw_kernel(SampleArgs a, int C, int ch
       uint64_t m = 0;
       for (int i = tid; i < r.V; i += kDraw) {
         const float z = clean(r.z[i]);
-        if (z != -INFINITY && rank_key(z, i) >= r.threshold) m += mass_of(exponent_of(z, r.ref, r.q.c));
+        if (z != -INFINITY && rank_key(z, i) >= r.threshold) m += r.mass_at(z);
       }
       scan(m);
       return scan.sum;
@@ -587,7 +670,7 @@ __global__ __launch_bounds__(kDraw) void draw_kernel(SampleArgs a, int C, int ch
       const int b = bin_of((float)depth);
       by_min = !by_p || (b < kBins - 1 && (double)sh.mass[b] < want);
       if (by_min) {
-        const float z = (float)((double)r.ref - depth * 0.5 / r.q.c);
+        const float z = (float)((double)r.ref - depth * 16 / r.q.c);
         by_min = whole || (z > -INFINITY && complete(z));
         if (by_min) by_p = false;  // top-p, if it is on, cuts deeper than min_p
       }
@@ -617,9 +700,9 @@ __global__ __launch_bounds__(kDraw) void draw_kernel(SampleArgs a, int C, int ch
         if (k < r.threshold || k == 0) continue;
         const float z = key_val(k);
         const double t = exponent_of(z, r.ref, r.q.c);
-        if (r.q.min_p > 0.0 && z != r.ref && exp2_64(t, 0) < r.q.min_p) continue;
+        if (r.q.min_p > 0.0 && z != r.ref && exp2_64(sh.parts, t) < r.q.min_p) continue;
         ++count;
-        atomicAdd((unsigned long long*)&sh.seg[key_id(k) / kSeg], (unsigned long long)mass_of(t));
+        atomicAdd((unsigned long long*)&sh.seg[key_id(k) / kSeg], (unsigned long long)mass_of(sh.parts, t));
       }
       scan(count);
       n_kept = (uint32_t)scan.sum;
@@ -689,7 +772,7 @@ __global__ __launch_bounds__(kDraw) void draw_kernel(SampleArgs a, int C, int ch
     a.tok[row] = id;
     if (a.kept) a.kept[row] = (int32_t)n_kept;
     if (a.logp)
-      a.logp[row] = (float)(exponent_of(clean(r.z[id]), ref, r.q.c) * 0.6931471805599453 - log((double)total * 0x1p-43));
+      a.logp[row] = (float)(exponent_of(clean(r.z[id]), ref, r.q.c) * (0.6931471805599453 / 32) - log((double)total * 0x1p-43));
   }
 }
 
