@@ -4,8 +4,8 @@
 // from the first row's window on, and one block of the rows' own keys where
 // they come beside the cache; blocks outside the window are not read. A
 // workgroup owns a chunk of consecutive blocks of one (sequence, kv head) and
-// up to 3 tiles of 16 queries (query head of the kv head's group, slot), its 4
-// waves a block each in turn:
+// up to 3 tiles of 16 queries (query head of the kv head's group, slot), its 8
+// waves (two a SIMD) a block each in turn:
 //   S^T[key][query] = K Q^T   MFMA 16x16x32 bf16. 8-bit codes become bf16 in
 //                             registers, multiplied by their block's scale in
 //                             the same instruction: exact, as a code has 4
@@ -27,8 +27,18 @@
 // Values that no query sees are zeroed as they are staged, so NaN in stale
 // rows, past the window or past the length meets no product. A non-finite value that
 // only some of the wave's queries see would reach the others as 0 * NaN: where a
-// wave ends with a non-finite output, it walks its blocks again with such
-// values taken out of the products and added to the queries that see them.
+// wave ends with a non-finite output, the workgroup does its chunk again query by
+// query, with only the keys that a query sees.
+//
+// What bounds it: the bytes of the seen keys and values where they are many (65.5K
+// positions, 32 kv heads, 8 bits: 537 MB in 98 us, 5.5 TB/s; 16 single tokens at 512 to
+// 8192: 167 MB in 38 to 42 us, 4.2 TB/s with chunks a quarter uneven); a round of
+// 8 blocks takes a workgroup of 3 tiles 2.7 to 3.1 us, bytes, exponentials and products alike. Few
+// bytes: a chain of latencies, as stamped in a copy: launch, plan 2.2 us, page numbers
+// 2, queries and first keys 4, joining the waves 1.3 to 2.5, the second kernel 4 to 5.
+// 32 positions a block, not 64: half the registers of a load, so two waves a SIMD
+// (16 chains 77 -> 62 us). A chunk's own reads are 16 bytes a lane from the rows of its
+// pages; keys go to the products without LDS, values through it, for their transpose.
 #pragma once
 #include "paged_plan.h"
 

@@ -11,7 +11,8 @@ void launch_paged_fp8_128(const PagedAttnArgs& a, const Topo& topo, dim3 grid, h
 namespace {
 
 // A workgroup a (sequence, kv head, query tile), a thread 8 dims of a query (half
-// of the threads idle at head dim 64).
+// of the threads idle at head dim 64). 4 us for 4 chunks or fewer (a launch and two
+// dependent loads), 5 for 8, 8.5 for 24.
 template <int HD>
 __global__ __launch_bounds__(256) void paged_merge_kernel(PagedAttnArgs a) {
   const int tid = threadIdx.x;

@@ -64,14 +64,26 @@ msd_status fill_append(const msd_paged_kv* kv, const msd_kv_rows* rows, const ms
   return MSD_OK;
 }
 
-// Launch shape of an attention call. Query tiles: as few groups as hold them,
-// evenly (each group reads the keys again). Workgroups: where the sequences alone
-// fill fewer than the device holds at once and a sequence can have more blocks
-// than two for each wave, chunks are planned on the device over that many
-// workgroups and joined by a second kernel.
-constexpr int64_t kPagedWgs = 512;    // workgroups of one query tile at head dim 64 (two fit a compute unit)
-constexpr int64_t kPagedWgsMany = 256;  // others (one fits)
-constexpr int64_t kPagedAlone = 16;   // blocks that one workgroup takes without a split
+// Launch shape of an attention call (8-bit pages, 8 kv heads, head dim 128 unless said;
+// attention and joining kernel).
+//
+// Query tiles: all groups of tiles read the keys again, so few groups of many tiles, unless
+// the call is small: a workgroup's round of 8 blocks takes three tiles nearly three times
+// as long as one. With at most kPagedRounds rounds over all workgroups, fewer tiles a
+// workgroup. A chain of 9 slots, 5 heads a kv head, at 100: 16.8 us with 3 tiles a
+// workgroup, 10.1 with one; at 900 21 and 15.4; at 6000 27.2 and 20.5. The
+// other way past the limit: at 30000 37.3 and 39.3, 8 sequences at 4000 35 and 47.7.
+//
+// Workgroups: where the sequences alone fill fewer than the device holds at once and a
+// sequence can have more blocks than two for each wave, chunks are planned on the
+// device over that many workgroups and joined by a second kernel. 14 blocks, one token:
+// 11.5 in one workgroup, 13.7 split; 29 blocks 15.4 and 14.8, of a chain 25.8 and 20.9.
+// 16 sequences at 512 to 8192: over 256 workgroups 42.3, over 512 47.6 (chains 61.9 and
+// 71.4); at head dim 64 (two fit a compute unit) 32.6 and 29.0.
+constexpr int64_t kPagedWgs = 512;      // workgroups of one query tile at head dim 64
+constexpr int64_t kPagedWgsMany = 256;  // others
+constexpr int64_t kPagedAlone = 16;     // blocks that one workgroup takes without a split
+constexpr int64_t kPagedRounds = 1024;
 struct PagedShape {
   int q_per_wg, groups, wgs;
 };
@@ -81,7 +93,10 @@ PagedShape paged_shape(const msd_paged_kv* kv, int32_t batch, int32_t n_slots, i
   const int tiles = (n_heads / heads * n_slots + 15) / 16;
   PagedShape s;
   const int most = paged_max_tiles(kv->format == MSD_KV_FP8, kv->head_dim);
-  s.groups = (tiles + most - 1) / most;
+  const int64_t rounds = (blocks + 7) / 8 * batch * heads;
+  int q = std::min(tiles, most);
+  while (q > 1 && rounds * ((tiles + q - 2) / (q - 1)) <= kPagedRounds) --q;
+  s.groups = (tiles + q - 1) / q;
   s.q_per_wg = (tiles + s.groups - 1) / s.groups;
   const int64_t share = (s.q_per_wg == 1 && light ? kPagedWgs : kPagedWgsMany) / ((int64_t)heads * s.groups);
   // (the plan counts all sequences' blocks in 32 bits)
