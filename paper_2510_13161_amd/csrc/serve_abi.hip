@@ -67,12 +67,14 @@ msd_status fill_append(const msd_paged_kv* kv, const msd_kv_rows* rows, const ms
 // Launch shape of an attention call (8-bit pages, 8 kv heads, head dim 128 unless said;
 // attention and joining kernel).
 //
-// Query tiles: all groups of tiles read the keys again, so few groups of many tiles, unless
-// the call is small: a workgroup's round of 8 blocks takes three tiles nearly three times
-// as long as one. With at most kPagedRounds rounds over all workgroups, fewer tiles a
-// workgroup. A chain of 9 slots, 5 heads a kv head, at 100: 16.8 us with 3 tiles a
-// workgroup, 10.1 with one; at 900 21 and 15.4; at 6000 27.2 and 20.5. The
-// other way past the limit: at 30000 37.3 and 39.3, 8 sequences at 4000 35 and 47.7.
+// Query tiles: groups of tiles read the keys again, so few groups of many tiles where
+// the keys are many; but a tile costs a workgroup 3.1 us of its own (queries, own
+// keys, joining the waves) beside 2.2 + 0.2 a tile for each round of 8 blocks (fitted to chains and
+// trees at 100 to 30000). The count with the least of that is taken. A chain of 9 slots,
+// 5 heads a kv head, at 100: 16.8 us with 3 tiles a workgroup, 10.1 with one; at 6000
+// 27.2 and 20.5; at 30000 37.3 and 39.3; 8 sequences at 4000 35 and 47.7, 16 at 300
+// (2 tiles) 16.8 and 22.3; a tree of
+// 25 slots at 8000 33.0 with 3, 29.4 with 2, 30.7 with one.
 //
 // Workgroups: where the sequences alone fill fewer than the device holds at once and a
 // sequence can have more blocks than two for each wave, chunks are planned on the
@@ -83,7 +85,6 @@ msd_status fill_append(const msd_paged_kv* kv, const msd_kv_rows* rows, const ms
 constexpr int64_t kPagedWgs = 512;      // workgroups of one query tile at head dim 64
 constexpr int64_t kPagedWgsMany = 256;  // others
 constexpr int64_t kPagedAlone = 16;     // blocks that one workgroup takes without a split
-constexpr int64_t kPagedRounds = 1024;
 struct PagedShape {
   int q_per_wg, groups, wgs;
 };
@@ -93,9 +94,16 @@ PagedShape paged_shape(const msd_paged_kv* kv, int32_t batch, int32_t n_slots, i
   const int tiles = (n_heads / heads * n_slots + 15) / 16;
   PagedShape s;
   const int most = paged_max_tiles(kv->format == MSD_KV_FP8, kv->head_dim);
-  const int64_t rounds = (blocks + 7) / 8 * batch * heads;
+  const int64_t rounds = (blocks + 7) / 8;
+  // 10 ns of a workgroup of q tiles: its chunk's rounds, those of all its turns on a full device
+  auto cost = [&](int q) {
+    const int64_t fit = kPagedWgsMany;  // two on a compute unit take turns
+    const int64_t all = (int64_t)batch * heads * ((tiles + q - 1) / q), chunks = std::max<int64_t>(1, fit / all);
+    return ((rounds + chunks - 1) / chunks * (225 + 22 * q) + 315 * q) * ((all + fit - 1) / fit);
+  };
   int q = std::min(tiles, most);
-  while (q > 1 && rounds * ((tiles + q - 2) / (q - 1)) <= kPagedRounds) --q;
+  for (int fewer = q - 1; fewer >= 1; --fewer)
+    if (cost(fewer) < cost(q)) q = fewer;
   s.groups = (tiles + q - 1) / q;
   s.q_per_wg = (tiles + s.groups - 1) / s.groups;
   const int64_t share = (s.q_per_wg == 1 && light ? kPagedWgs : kPagedWgsMany) / ((int64_t)heads * s.groups);
