@@ -366,6 +366,46 @@ def test_attention(fmt, hd, H, Hk, page, lens, block, own, counts, rot, window, 
     assert torch.equal(out, again)
 
 
+@pytest.mark.parametrize("fmt,hd,B,L,block,rot,window", [
+    ("bf16", 128, 16, 600, 9, None, 0), ("bf16", 128, 1, 4033, tree(4, 6), ("half", 128), 0),
+    ("fp8", 128, 32, 600, 9, ("half", 128), 0), ("fp8", 128, 16, 600, 9, None, 0), ("fp8", 128, 4, 4000, 9, None, 0),
+    ("fp8", 128, 12, 3000, 6, ("interleaved", 64), 1000), ("bf16", 64, 32, 600, 9, ("half", 64), 0),
+    ("fp8", 64, 32, 600, 9, None, 0), ("fp8", 64, 4, 4000, 9, ("half", 64), 0), ("bf16", 64, 2, 4000, tree(4, 6), None, 500)])
+def test_attention_of_calls_that_fill_the_device(fmt, hd, B, L, block, rot, window):
+    """Several query tiles a workgroup: many sequences, or long ones."""
+    parent = [-1] + list(range(block - 1)) if isinstance(block, int) else block
+    n, Hk, H = len(parent), 8, 40
+    g = gen(23)
+    lens = [L] + torch.randint(1, L + 1, (B - 1,), generator=g).tolist()
+    c = make_cache(fmt, 1, Hk, hd, 64, lens, n, 24)
+    q, kn, vn = normal(g, B, n, H, hd), normal(g, B, n, Hk, hd), normal(g, B, n, Hk, hd)
+    layout, rd = rot or ("half", 0)
+    tab = R.table(c.c.max_pages * 64, rd) if rot else None
+    counts = [n] + torch.randint(0, n + 1, (B - 1,), generator=g).tolist()
+    out = run_attention(c, q, kn, vn, parent=None if isinstance(block, int) else parent, counts=counts, tab=tab, layout=layout,
+                        window=window, sinks=4 if window else 0)
+    check(out, *reference(c, 0, q, kn, vn, lens, parent, counts, tab, layout, window, 4 if window else 0, hd ** -0.5))
+    assert status(c) == 0
+
+
+@pytest.mark.parametrize("fmt,hd,B,L", [("bf16", 128, 16, 600), ("fp8", 128, 32, 600), ("fp8", 128, 4, 4000), ("bf16", 64, 32, 600),
+                                        ("fp8", 64, 32, 600)])
+def test_non_finite_rows_among_several_query_tiles(fmt, hd, B, L):
+    """The last slot's own key and value are infinite and NaN: only that slot sees them."""
+    n, Hk, H = 9, 8, 40
+    g = gen(25)
+    lens = [L] + torch.randint(1, L + 1, (B - 1,), generator=g).tolist()
+    c = make_cache(fmt, 1, Hk, hd, 64, lens, n, 26)
+    q, kn, vn = normal(g, B, n, H, hd), normal(g, B, n, Hk, hd), normal(g, B, n, Hk, hd)
+    outs, tols = reference(c, 0, q, kn, vn, lens, list(range(-1, n - 1)), None, None, "half", 0, 0, hd ** -0.5)
+    kn[::2, n - 1], vn[::2, n - 1] = math.inf, math.nan
+    out = run_attention(c, q, kn, vn).double().cpu()
+    for b in range(B):
+        m = n - 1 if b % 2 == 0 else n
+        assert bool(((out[b, :m] - outs[b][:m]).abs() <= tols[b][:m]).all()), b
+        assert b % 2 or bool(torch.isnan(out[b, n - 1]).any())
+
+
 @pytest.mark.parametrize("fmt", ["bf16", "fp8"])
 def test_attention_of_long_contexts_in_parts(fmt):
     """Enough keys for the work to be split and joined: lengths that differ, one short, one of a single token."""
